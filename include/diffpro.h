@@ -258,6 +258,83 @@ int dp_ln_modulate_daq(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, co
                        float* s_a, dp_stream stream);
 
 /*
+ * Softmax attention, the operator between a block's qkv and projection linears (Step 3 keeps it in higher precision: bf16 in
+ * and out, scores, softmax and sums in fp32, the weights rounded to bf16 for the tensor core like every bf16 operand here).
+ * Sequence s has queries i = 0 .. Lq - 1 and keys j = 0 .. Lk - 1; query i stands at key position pos(i) = i + Lk - Lq (the
+ * last query at the last key, which also serves new tokens behind cached ones). Head h reads key head h / (heads / kv_heads).
+ *
+ *     t_ij = scale * q_i . k_j
+ *     cap > 0:        t_ij = cap * tanh(t_ij / cap)
+ *     slopes:         t_ij -= slopes[h] * |pos(i) - j|
+ *     DP_MASK_CAUSAL: key j is visible to query i where j <= pos(i) or j < prefix[s]; DP_MASK_NONE: everywhere
+ *     y_i = sum_j w_ij v_j,  w_ij = exp(t_ij) / sum_j exp(t_ij) over the visible keys;  no key visible: y_i = 0
+ *
+ * Sequences are packed: sequence s has the rows q_start[s] .. q_start[s + 1] - 1 of q and y and k_start[s] .. k_start[s + 1]
+ * - 1 of k and v, so documents of one buffer do not see each other. Rows of other sequences, between sequences and behind
+ * the last one are not read into any result, whatever they hold, and rows of y there stay as they are. Without offsets all
+ * sequences have max_q queries and max_k keys. Within a sequence, q and k may hold anything where the mask hides the pair,
+ * but v has to be finite: a value that is not reaches rows of the same sequence and head that do not see it.
+ */
+#define DP_MASK_NONE 0
+#define DP_MASK_CAUSAL 1
+typedef struct dp_attn {
+  int32_t heads, kv_heads;       /* heads a multiple of kv_heads                                              */
+  int32_t head_dim;              /* a multiple of 8, at most 128                                              */
+  int32_t n_seq;
+  int64_t max_q, max_k;          /* longest sequence, queries and keys. Queries beyond max_q are left out; max_k is
+                                    a hint for cutting the work where there are offsets                        */
+  int64_t q_head_stride, k_head_stride, v_head_stride, y_head_stride; /* elements between heads; 0: head_dim   */
+  const int32_t* q_start;        /* device: [n_seq + 1], ascending, or NULL. Offsets beyond Mq / Mk are cut there */
+  const int32_t* k_start;        /* device: [n_seq + 1], with q_start                                         */
+  const int32_t* prefix;         /* device: [n_seq] or NULL (0); DP_MASK_CAUSAL only                          */
+  const float* slopes;           /* device: [heads] or NULL (no distance bias)                                */
+  float scale, cap;              /* finite, >= 0; cap 0: scores are not capped                                */
+  int32_t mask;                  /* DP_MASK_NONE, DP_MASK_CAUSAL                                              */
+  int32_t reserved;
+} dp_attn;
+
+/*
+ *   a          : host pointer, read during the call
+ *   q, ldq, Mq : bf16, token t and head h at q + t * ldq + h * q_head_stride, Mq rows in the buffer; y likewise
+ *   k, v       : bf16, Mk rows
+ * (columns of one qkv buffer: q, k, v point into it with the same ld). Pointers 16-byte aligned, strides multiples of 8 and
+ * at least head_dim; y overlaps neither an input nor itself. Fewer than 2^31 - 1024 rows. flags: DP_FLAG_NO_PDL,
+ * DP_FLAG_FORCE_SIMT (the kernel for few queries, whatever max_q is), DP_FLAG_FORCE_MMA (the tcgen05 kernel). No scratch
+ * memory, nothing kept between calls; results do not depend on what runs beside the call. Enqueues one kernel. Errors:
+ * DP_ERR_INVALID_ARG, DP_ERR_SHAPE, DP_ERR_ALIGN, DP_ERR_ARCH.
+ */
+int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const void* k, int64_t ldk, const void* v,
+                 int64_t ldv, int64_t Mk, void* y, int64_t ldy, int32_t* device_status, uint32_t flags, dp_stream stream);
+
+/*
+ * Group normalisation of channels-last feature maps with an activation: what stands in front of a U-Net block's projections
+ * (the method quantizes those like a DiT's linears; Step 3 keeps normalization in higher precision). x is bf16
+ * [n_samples * rows][ldx], `groups` groups of C / groups neighbouring channels; over the rows * C / groups values of a sample's
+ * group
+ *     mean, var (biased), from fp32 sums of the values less one of them, joined in double
+ *     h = (x - mean) / sqrt(var + eps) * gamma[c] + beta[c]                        fp32
+ *     act(h): DP_ACT_NONE h, DP_ACT_SILU h / (1 + exp(-h))                          fp32
+ * dp_group_norm writes y = bf16(act(h)) [n_samples * rows][ldy]; dp_group_norm_daq writes Eq. "daq" of act(h), codes
+ * [..][ldq] and a scale per row as dp_daq_quantize, for dp_wq_linear(w, q, ldq, s_a, ...): the normalized values exist only
+ * in fp32 then.
+ *   gamma, beta : device bf16 [C], 16-byte aligned, or both NULL (1 and 0)
+ *   workspace   : >= dp_group_norm_workspace(...) bytes, 256-byte aligned, contents undefined before and after; one call at a
+ *                 time may use it
+ * C a multiple of 8, at most 4608, and of `groups` (at most 1024); x and the output 16-byte aligned, ldx and ldy multiples of
+ * 8, ldq of 16; the output does not overlap x; at most 2^31 rows and 2^23 samples. n_samples == 0 or rows == 0 is a no-op.
+ * Errors: DP_ERR_INVALID_ARG, DP_ERR_SHAPE, DP_ERR_ALIGN, DP_ERR_WORKSPACE, DP_ERR_ARCH.
+ */
+#define DP_ACT_NONE 0
+#define DP_ACT_SILU 1
+size_t dp_group_norm_workspace(int64_t n_samples, int64_t rows, int32_t C, int32_t groups);
+int dp_group_norm(const void* x, int64_t n_samples, int64_t rows, int32_t C, int64_t ldx, int32_t groups, const void* gamma,
+                  const void* beta, float eps, int32_t act, void* y, int64_t ldy, void* workspace, size_t workspace_bytes,
+                  dp_stream stream);
+int dp_group_norm_daq(const void* x, int64_t n_samples, int64_t rows, int32_t C, int64_t ldx, int32_t groups,
+                      const void* gamma, const void* beta, float eps, int32_t act, int8_t* q, int64_t ldq, float* s_a,
+                      void* workspace, size_t workspace_bytes, dp_stream stream);
+
+/*
  * The residual connection around a wrapped linear, taken into its epilogue (Step 3 keeps residual
  * adds in higher precision; a DiT block adds its attention projection and MLP output to the token
  * stream scaled by an adaLN gate per sample and channel). With lin[m][n] the fp32 value that

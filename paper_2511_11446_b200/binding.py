@@ -27,6 +27,8 @@ DP_FLAG_UNPACK_FIRST, DP_FLAG_NO_UNPACK_FIRST = 0x80000, 0x100000
 DP_FLAG_ACT_STATIONARY, DP_FLAG_NO_ACT_STATIONARY = 0x200000, 0x400000
 DP_FLAG_TILE_N_MASK = 0x700
 DP_PLAN_SAME_X, DP_PLAN_SAME_Y = 1, 2
+DP_MASK_NONE, DP_MASK_CAUSAL = 0, 1
+DP_ACT_NONE, DP_ACT_SILU = 0, 1
 
 
 def DP_FLAG_TILE_N(bn: int) -> int:
@@ -34,7 +36,7 @@ def DP_FLAG_TILE_N(bn: int) -> int:
 
 DP_STATIC_SCRATCH_BYTES = 10 << 20
 
-EXPORTS = ["dp_daq_quantize", "dp_daq_quantize_robust", "dp_wq_linear_workspace", "dp_wq_linear_workspace_grouped", "dp_wq_linear", "dp_wq_linear_static", "dp_wq_linear_residual", "dp_ln_modulate_daq", "dp_plan_create",
+EXPORTS = ["dp_daq_quantize", "dp_daq_quantize_robust", "dp_wq_linear_workspace", "dp_wq_linear_workspace_grouped", "dp_wq_linear", "dp_wq_linear_static", "dp_wq_linear_residual", "dp_ln_modulate_daq", "dp_attention", "dp_group_norm_workspace", "dp_group_norm", "dp_group_norm_daq", "dp_plan_create",
            "dp_plan_workspace", "dp_plan_layer_variant", "dp_plan_layer_unpack_first", "dp_plan_layer_unit", "dp_plan_set_layer_flags", "dp_plan_set_daq", "dp_plan_destroy", "dp_plan_run", "dp_plan_x_bytes",
            "dp_plan_run_host", "dp_plan_phase_a", "dp_layer_latency_us", "dp_pack_weights_host", "dp_clip_rank", "dp_debug_skip_stage_load",
            "dp_status_string",
@@ -49,6 +51,14 @@ class dp_weight(C.Structure):
 class dp_debug(C.Structure):
     _fields_ = [("q", C.c_void_p), ("ldq", C.c_int64), ("s_a", C.c_void_p), ("acc", C.c_void_p),
                 ("ldacc", C.c_int64)]
+
+
+class dp_attn(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_seq", C.c_int32),
+                ("max_q", C.c_int64), ("max_k", C.c_int64), ("q_head_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_head_stride", C.c_int64), ("y_head_stride", C.c_int64), ("q_start", C.c_void_p),
+                ("k_start", C.c_void_p), ("prefix", C.c_void_p), ("slopes", C.c_void_p), ("scale", C.c_float),
+                ("cap", C.c_float), ("mask", C.c_int32), ("reserved", C.c_int32)]
 
 
 class dp_phase_a_problem(C.Structure):
@@ -101,6 +111,14 @@ def lib():
                                    C.POINTER(dp_debug), C.c_void_p, C.c_uint32, C.c_void_p]
         L.dp_ln_modulate_daq.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
                                          C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.dp_attention.argtypes = [C.POINTER(dp_attn), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                   C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_uint32, C.c_void_p]
+        L.dp_group_norm_workspace.restype = C.c_size_t
+        L.dp_group_norm_workspace.argtypes = [C.c_int64, C.c_int64, C.c_int32, C.c_int32]
+        gn = [C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
+              C.c_void_p, C.c_int64]
+        L.dp_group_norm.argtypes = gn + [C.c_void_p, C.c_size_t, C.c_void_p]
+        L.dp_group_norm_daq.argtypes = gn + [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.dp_wq_linear_residual.argtypes = [C.POINTER(dp_weight), C.c_void_p, C.c_int64, C.c_int64, C.POINTER(dp_residual),
                                             C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p, C.c_uint32,
                                             C.c_void_p]
@@ -152,7 +170,8 @@ def _calls():
             raise RuntimeError("the call module is missing: build it with `python -m paper_2511_11446_b200.build`") from e
         addr = lambda f: C.cast(f, C.c_void_p).value
         m.bind(addr(L.dp_wq_linear), addr(L.dp_wq_linear_residual), addr(L.dp_daq_quantize), addr(L.dp_ln_modulate_daq),
-               torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, dp_weight, dp_debug, C.ArgumentError)
+               addr(L.dp_attention), addr(L.dp_group_norm), addr(L.dp_group_norm_daq), torch.cuda.current_device,
+               torch._C._cuda_getCurrentRawStream, dp_weight, dp_debug, dp_attn, C.ArgumentError)
         _call = m
     return _call
 
@@ -204,6 +223,36 @@ def dp_ln_modulate_daq(x, M, K, ldx, shift, scale, rows_per_sample, eps, q, ldq,
     """LayerNorm + adaLN modulation + DAQ of bf16 tokens in one pass (shift, scale may both be None)."""
     _check((_call or _calls()).ln_modulate_daq(x, M, K, ldx, shift, scale, rows_per_sample, eps, q, ldq, s_a, stream),
            "dp_ln_modulate_daq")
+
+
+def make_attn(heads, kv_heads, head_dim, n_seq, max_q, max_k, scale, q_start=None, k_start=None, mask=DP_MASK_NONE,
+              prefix=None, cap=0.0, slopes=None, q_head_stride=0, k_head_stride=0, v_head_stride=0,
+              y_head_stride=0) -> dp_attn:
+    """The description of an attention call; the device tensors it names have to outlive its use."""
+    return dp_attn(heads, kv_heads, head_dim, n_seq, max_q, max_k, q_head_stride, k_head_stride, v_head_stride,
+                   y_head_stride, _ptr(q_start), _ptr(k_start), _ptr(prefix), _ptr(slopes), scale, cap, mask, 0)
+
+
+def dp_attention(a: dp_attn, q, ldq, Mq, k, ldk, v, ldv, Mk, y, ldy, device_status=None, flags=0, stream=None):
+    """Softmax attention of packed sequences on bf16 projections (columns of one buffer or buffers of their own)."""
+    _check((_call or _calls()).attention(a, q, ldq, Mq, k, ldk, v, ldv, Mk, y, ldy, device_status, flags, stream),
+           "dp_attention")
+
+
+def dp_group_norm_workspace(n_samples, rows, C_, groups) -> int:
+    return int(lib().dp_group_norm_workspace(n_samples, rows, C_, groups))
+
+
+def dp_group_norm(x, n_samples, rows, C_, ldx, groups, gamma, beta, eps, act, y, ldy, workspace, stream=None):
+    """Group normalisation + activation of channels-last maps to bf16 (gamma, beta may both be None)."""
+    _check((_call or _calls()).group_norm(x, n_samples, rows, C_, ldx, groups, gamma, beta, eps, act, y, ldy, workspace,
+                                          stream), "dp_group_norm")
+
+
+def dp_group_norm_daq(x, n_samples, rows, C_, ldx, groups, gamma, beta, eps, act, q, ldq, s_a, workspace, stream=None):
+    """The same to int8 codes and a scale per row, for dp_wq_linear."""
+    _check((_call or _calls()).group_norm_daq(x, n_samples, rows, C_, ldx, groups, gamma, beta, eps, act, q, ldq, s_a,
+                                              workspace, stream), "dp_group_norm_daq")
 
 
 class dp_residual(C.Structure):

@@ -9,6 +9,7 @@
 #include <queue>
 #include <vector>
 
+#include "attn.cuh"
 #include "dp_common.cuh"
 #include "dp_internal.h"
 
@@ -560,6 +561,142 @@ extern "C" int dp_ln_modulate_daq(const void* x, int64_t M, int64_t K, int64_t l
   if (st != DP_OK) return st;
   return launch_ln_modulate_daq(x, M, K, ldx, shift, scale, shift ? rows_per_sample : 1, eps, q, ldq, s_a,
                                 static_cast<cudaStream_t>(stream), true);
+}
+
+// ---- attention --------------------------------------------------------------------------------------
+static bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+// `rows` x `heads` vectors of D elements of 16 bits.
+struct AttnRange {
+  const void* p;
+  int64_t rows, ld;
+  int32_t heads;
+  int64_t hs;
+  int32_t D;
+  int64_t bytes() const { return rows < 1 ? 0 : 2 * ((rows - 1) * ld + (heads - 1) * hs + D); }
+  int64_t width() const { return (heads - 1) * hs + D; }
+};
+static bool attn_overlap(const AttnRange& a, const AttnRange& b) {
+  if (!ranges_meet(a.p, a.bytes(), b.p, b.bytes())) return false;
+  if (a.ld != b.ld || a.width() > a.ld || b.width() > b.ld) return true;
+  // columns of one buffer: apart where neither reaches the other within a row
+  const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(a.p));
+  const int64_t off = ((d / 2) % a.ld + a.ld) % a.ld;
+  return off < a.width() || off + b.width() > a.ld;
+}
+
+extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const void* k, int64_t ldk,
+                            const void* v, int64_t ldv, int64_t Mk, void* y, int64_t ldy, int32_t* device_status,
+                            uint32_t flags, dp_stream stream) {
+  if (!a) return fail(DP_ERR_INVALID_ARG, "dp_attn is NULL");
+  if (flags & ~(DP_FLAG_FORCE_SIMT | DP_FLAG_FORCE_MMA | DP_FLAG_NO_PDL) ||
+      (flags & (DP_FLAG_FORCE_SIMT | DP_FLAG_FORCE_MMA)) == (DP_FLAG_FORCE_SIMT | DP_FLAG_FORCE_MMA))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: flags 0x%x", flags);
+  const int32_t H = a->heads, KV = a->kv_heads, D = a->head_dim;
+  if (H < 1 || KV < 1 || H % KV) return fail(DP_ERR_SHAPE, "dp_attention: heads=%d kv_heads=%d", H, KV);
+  if (D < 8 || D > 128 || D % 8) return fail(DP_ERR_SHAPE, "dp_attention: head_dim=%d must be a multiple of 8, at most 128", D);
+  constexpr int64_t kMaxRows = (1ll << 31) - 1024;
+  if (a->n_seq < 0 || a->max_q < 0 || a->max_k < 0 || Mq < 0 || Mk < 0 || Mq > kMaxRows || Mk > kMaxRows ||
+      a->max_q > kMaxRows || a->max_k > kMaxRows)
+    return fail(DP_ERR_SHAPE, "dp_attention: n_seq=%d max_q=%lld max_k=%lld Mq=%lld Mk=%lld", a->n_seq, (long long)a->max_q,
+                (long long)a->max_k, (long long)Mq, (long long)Mk);
+  if ((a->q_start == nullptr) != (a->k_start == nullptr))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: q_start and k_start come together");
+  if (a->q_start == nullptr && (a->n_seq * a->max_q > Mq || a->n_seq * a->max_k > Mk))
+    return fail(DP_ERR_SHAPE, "dp_attention: n_seq sequences of max_q, max_k rows do not fit Mq, Mk");
+  if (a->mask != DP_MASK_NONE && a->mask != DP_MASK_CAUSAL) return fail(DP_ERR_INVALID_ARG, "dp_attention: mask=%d", a->mask);
+  if (a->prefix != nullptr && a->mask != DP_MASK_CAUSAL)
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: a prefix goes with DP_MASK_CAUSAL");
+  if (!(a->scale >= 0.0f) || !(a->scale <= 3.0e38f) || !(a->cap >= 0.0f) || !(a->cap <= 1.0e30f))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: scale=%g cap=%g must be finite and not negative", a->scale, a->cap);
+  const int64_t qh = a->q_head_stride ? a->q_head_stride : D, kh = a->k_head_stride ? a->k_head_stride : D;
+  const int64_t vh = a->v_head_stride ? a->v_head_stride : D, yh = a->y_head_stride ? a->y_head_stride : D;
+  constexpr int64_t kMaxStride = 1ll << 38;  // elements: a tensor map's strides stay below 2^40 bytes
+  for (int64_t s : {ldq, ldk, ldv, ldy, qh, kh, vh, yh})
+    if (s < D || s > kMaxStride) return fail(DP_ERR_SHAPE, "dp_attention: a stride of %lld elements for vectors of %d", (long long)s, D);
+  if (a->n_seq == 0 || a->max_q == 0 || Mq == 0) return DP_OK;
+  if (H > 1 && ldy < (H - 1) * yh + D && yh < (Mq - 1) * ldy + D)
+    return fail(DP_ERR_SHAPE, "dp_attention: heads and rows of y overlap");
+  if (!q || !y || (Mk > 0 && (!k || !v))) return fail(DP_ERR_INVALID_ARG, "dp_attention: NULL argument");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(y) || (ldq % 8) || (ldk % 8) || (ldv % 8) || (ldy % 8) ||
+      (qh % 8) || (kh % 8) || (vh % 8) || (yh % 8))
+    return fail(DP_ERR_ALIGN, "dp_attention: pointers and strides must be 16-byte aligned");
+  for (const void* p : {static_cast<const void*>(a->q_start), static_cast<const void*>(a->k_start),
+                        static_cast<const void*>(a->prefix), static_cast<const void*>(a->slopes)})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(DP_ERR_ALIGN, "dp_attention: offsets and slopes must be 4-byte aligned");
+  const AttnRange yr{y, Mq, ldy, H, yh, D};
+  if (attn_overlap({q, Mq, ldq, H, qh, D}, yr) || attn_overlap({k, Mk, ldk, KV, kh, D}, yr) || attn_overlap({v, Mk, ldv, KV, vh, D}, yr))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: y overlaps an input");
+  int st = check_device();
+  if (st != DP_OK) return st;
+  AttnParams p{};
+  p.q = static_cast<const uint16_t*>(q);
+  p.k = static_cast<const uint16_t*>(k);
+  p.v = static_cast<const uint16_t*>(v);
+  p.y = static_cast<uint16_t*>(y);
+  p.ldq = ldq, p.ldk = ldk, p.ldv = ldv, p.ldy = ldy;
+  p.q_hs = qh, p.k_hs = kh, p.v_hs = vh, p.y_hs = yh;
+  p.Mq = Mq, p.Mk = Mk;
+  p.H = H, p.KV = KV, p.D = D;
+  p.n_seq = a->n_seq;
+  p.max_q = static_cast<int32_t>(a->max_q), p.max_k = static_cast<int32_t>(a->max_k);
+  p.q_start = a->q_start, p.k_start = a->k_start, p.prefix = a->prefix, p.slopes = a->slopes;
+  const double log2e = 1.4426950408889634074;
+  p.scale = static_cast<float>(a->scale * log2e);
+  p.cap = static_cast<float>(a->cap * log2e);
+  p.scale_by_cap = a->cap != 0.0f ? static_cast<float>(2.0 * log2e * a->scale / a->cap) : 0.0f;
+  p.causal = a->mask == DP_MASK_CAUSAL;
+  p.status = device_status;
+  return launch_attn_rows(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));
+}
+
+// ---- group normalisation ------------------------------------------------------------------------------
+extern "C" size_t dp_group_norm_workspace(int64_t n_samples, int64_t rows, int32_t C, int32_t groups) {
+  (void)C;
+  return group_norm_workspace(n_samples, rows, groups < 1 ? 1 : groups);
+}
+
+static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, int32_t C, int64_t ldx, int32_t G,
+                      const void* gamma, const void* beta, float eps, int32_t act, void* out, int64_t ldo, int out_size,
+                      float* s_a, void* workspace, size_t workspace_bytes, dp_stream stream) {
+  if (n < 0 || rows < 0 || C < 8 || C > 4608 || C % 8 || G < 1 || C % G)
+    return fail(DP_ERR_SHAPE, "%s: n_samples=%lld rows=%lld C=%d groups=%d", name, (long long)n, (long long)rows, C, G);
+  constexpr int64_t kMaxRows = 1ll << 31;
+  if (G > 1024 || rows > kMaxRows || n > (1 << 23) || n * (rows > 0 ? rows : 1) > kMaxRows)
+    return fail(DP_ERR_SHAPE, "%s: n_samples=%lld rows=%lld groups=%d", name, (long long)n, (long long)rows, G);
+  if ((gamma == nullptr) != (beta == nullptr)) return fail(DP_ERR_INVALID_ARG, "%s: gamma and beta come together", name);
+  if (!(eps >= 0.0f)) return fail(DP_ERR_INVALID_ARG, "%s: eps must be >= 0", name);
+  if (act != DP_ACT_NONE && act != DP_ACT_SILU) return fail(DP_ERR_INVALID_ARG, "%s: act=%d", name, act);
+  if (n == 0 || rows == 0) return DP_OK;
+  if (!x || !out || (out_size == 1 && !s_a)) return fail(DP_ERR_INVALID_ARG, "%s: NULL argument", name);
+  if (ldx < C || ldo < C) return fail(DP_ERR_SHAPE, "%s: leading dimension smaller than the row", name);
+  if (!aligned16(x) || !aligned16(out) || (ldx % 8) || (ldo * out_size % 16) || !aligned16(gamma) || !aligned16(beta) ||
+      (reinterpret_cast<uintptr_t>(s_a) & 3u))
+    return fail(DP_ERR_ALIGN, "%s: pointers and pitches must be 16-byte aligned", name);
+  if (!workspace || workspace_bytes < group_norm_workspace(n, rows, G) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return fail(DP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, 256-byte aligned", name, group_norm_workspace(n, rows, G));
+  if (ranges_meet(x, 2 * ((n * rows - 1) * ldx + C), out, out_size * ((n * rows - 1) * ldo + C)))
+    return fail(DP_ERR_INVALID_ARG, "%s: the output overlaps x", name);
+  int st = check_device();
+  if (st != DP_OK) return st;
+  return launch_group_norm(x, n, rows, C, ldx, G, gamma, beta, eps, act == DP_ACT_SILU, out_size == 2 ? out : nullptr, ldo,
+                           out_size == 1 ? static_cast<int8_t*>(out) : nullptr, ldo, s_a, workspace,
+                           static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int dp_group_norm(const void* x, int64_t n_samples, int64_t rows, int32_t C, int64_t ldx, int32_t groups,
+                             const void* gamma, const void* beta, float eps, int32_t act, void* y, int64_t ldy,
+                             void* workspace, size_t workspace_bytes, dp_stream stream) {
+  return group_norm("dp_group_norm", x, n_samples, rows, C, ldx, groups, gamma, beta, eps, act, y, ldy, 2, nullptr, workspace,
+                    workspace_bytes, stream);
+}
+extern "C" int dp_group_norm_daq(const void* x, int64_t n_samples, int64_t rows, int32_t C, int64_t ldx, int32_t groups,
+                                 const void* gamma, const void* beta, float eps, int32_t act, int8_t* q, int64_t ldq,
+                                 float* s_a, void* workspace, size_t workspace_bytes, dp_stream stream) {
+  return group_norm("dp_group_norm_daq", x, n_samples, rows, C, ldx, groups, gamma, beta, eps, act, q, ldq, 1, s_a, workspace,
+                    workspace_bytes, stream);
 }
 
 extern "C" int dp_wq_linear_residual(const dp_weight* w, const void* x_bf16, int64_t ldx, int64_t M,

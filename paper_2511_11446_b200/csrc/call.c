@@ -16,8 +16,14 @@ static int (*f_residual)(const dp_weight*, const void*, int64_t, int64_t, const 
 static int (*f_daq)(const void*, int64_t, int64_t, int64_t, int8_t*, int64_t, float*, int32_t*, dp_stream);
 static int (*f_ln)(const void*, int64_t, int64_t, int64_t, const void*, const void*, int64_t, float, int8_t*, int64_t,
                    float*, dp_stream);
+static int (*f_attn)(const dp_attn*, const void*, int64_t, int64_t, const void*, int64_t, const void*, int64_t, int64_t, void*,
+                     int64_t, int32_t*, uint32_t, dp_stream);
+static int (*f_gn)(const void*, int64_t, int64_t, int32_t, int64_t, int32_t, const void*, const void*, float, int32_t, void*,
+                   int64_t, void*, size_t, dp_stream);
+static int (*f_gn_daq)(const void*, int64_t, int64_t, int32_t, int64_t, int32_t, const void*, const void*, float, int32_t,
+                       int8_t*, int64_t, float*, void*, size_t, dp_stream);
 static PyObject *g_get_device, *g_get_stream; /* torch.cuda.current_device, torch._C._cuda_getCurrentRawStream */
-static PyObject *g_weight, *g_debug, *g_arg_error; /* the ctypes structures dp_weight and dp_debug, ctypes.ArgumentError */
+static PyObject *g_weight, *g_debug, *g_attn, *g_arg_error; /* the ctypes structures dp_weight, dp_debug, dp_attn, ctypes.ArgumentError */
 static PyObject *s_data_ptr, *s_nbytes, *s_cuda_stream;
 
 /* The converters leave a Python error behind; callers look once, before the call, with PyErr_Occurred. */
@@ -168,25 +174,93 @@ static PyObject* ln_modulate_daq(PyObject* self, PyObject* const* a, Py_ssize_t 
   return PyLong_FromLong(st);
 }
 
-/* (addresses of dp_wq_linear, dp_wq_linear_residual, dp_daq_quantize, dp_ln_modulate_daq, device getter, stream getter,
- * dp_weight, dp_debug, ctypes.ArgumentError) */
+/* (attn, q, ldq, Mq, k, ldk, v, ldv, Mk, y, ldy, device_status, flags, stream) */
+static PyObject* attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  (void)self;
+  if (!args_ok(n, 14)) return NULL;
+  const dp_attn* at = as_struct(a[0], g_attn);
+  const void* q = tensor_ptr(a[1]);
+  const int64_t ldq = as_i64(a[2]), Mq = as_i64(a[3]);
+  const void* k = tensor_ptr(a[4]);
+  const int64_t ldk = as_i64(a[5]);
+  const void* v = tensor_ptr(a[6]);
+  const int64_t ldv = as_i64(a[7]), Mk = as_i64(a[8]);
+  void* y = tensor_ptr(a[9]);
+  const int64_t ldy = as_i64(a[10]);
+  int32_t* status = tensor_ptr(a[11]);
+  const uint32_t flags = as_flags(a[12]);
+  const dp_stream s = stream_of(a[13]);
+  if (PyErr_Occurred()) return NULL;
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = f_attn(at, q, ldq, Mq, k, ldk, v, ldv, Mk, y, ldy, status, flags, s);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(st);
+}
+
+static int32_t as_i32(PyObject* o) {
+  const int64_t v = as_i64(o);
+  if (!PyErr_Occurred() && v != (int32_t)v) PyErr_Format(PyExc_OverflowError, "%lld does not fit 32 bits", (long long)v);
+  return (int32_t)v;
+}
+
+/* (x, n_samples, rows, C, ldx, groups, gamma, beta, eps, act, y, ldy, workspace, stream), or with codes
+ * (..., act, q, ldq, s_a, workspace, stream) */
+static PyObject* group_norm_call(PyObject* const* a, Py_ssize_t n, int codes) {
+  if (!args_ok(n, 14 + codes)) return NULL;
+  const void* x = tensor_ptr(a[0]);
+  const int64_t ns = as_i64(a[1]), rows = as_i64(a[2]);
+  const int32_t C = as_i32(a[3]);
+  const int64_t ldx = as_i64(a[4]);
+  const int32_t G = as_i32(a[5]);
+  const void *gamma = tensor_ptr(a[6]), *beta = tensor_ptr(a[7]);
+  const double eps = PyErr_Occurred() ? 0.0 : PyFloat_AsDouble(a[8]);
+  const int32_t act = as_i32(a[9]);
+  void* out = tensor_ptr(a[10]);
+  const int64_t ldo = as_i64(a[11]);
+  float* sa = codes ? tensor_ptr(a[12]) : NULL;
+  void* ws = tensor_ptr(a[12 + codes]);
+  const size_t wsb = tensor_bytes(a[12 + codes]);
+  const dp_stream s = stream_of(a[13 + codes]);
+  if (PyErr_Occurred()) return NULL;
+  int st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = codes ? f_gn_daq(x, ns, rows, C, ldx, G, gamma, beta, (float)eps, act, out, ldo, sa, ws, wsb, s)
+             : f_gn(x, ns, rows, C, ldx, G, gamma, beta, (float)eps, act, out, ldo, ws, wsb, s);
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(st);
+}
+static PyObject* group_norm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  (void)self;
+  return group_norm_call(a, n, 0);
+}
+static PyObject* group_norm_daq(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  (void)self;
+  return group_norm_call(a, n, 1);
+}
+
+/* (addresses of dp_wq_linear, dp_wq_linear_residual, dp_daq_quantize, dp_ln_modulate_daq, dp_attention, dp_group_norm,
+ * dp_group_norm_daq, device getter, stream getter, dp_weight, dp_debug, dp_attn, ctypes.ArgumentError) */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
   (void)self;
-  if (n != 9 || !PyType_Check(a[6]) || !PyType_Check(a[7])) {
-    PyErr_SetString(PyExc_TypeError, "bind takes four addresses, two callables and three types");
+  if (n != 13 || !PyType_Check(a[9]) || !PyType_Check(a[10]) || !PyType_Check(a[11])) {
+    PyErr_SetString(PyExc_TypeError, "bind takes seven addresses, two callables and four types");
     return NULL;
   }
-  void* p[4];
-  for (int i = 0; i < 4; ++i) p[i] = as_addr(a[i]);
+  void* p[7];
+  for (int i = 0; i < 7; ++i) p[i] = as_addr(a[i]);
   if (PyErr_Occurred()) return NULL;
   *(void**)&f_linear = p[0];
   *(void**)&f_residual = p[1];
   *(void**)&f_daq = p[2];
   *(void**)&f_ln = p[3];
-  PyObject** keep[5] = {&g_get_device, &g_get_stream, &g_weight, &g_debug, &g_arg_error};
-  for (int i = 0; i < 5; ++i) {
-    Py_INCREF(a[4 + i]);
-    Py_XSETREF(*keep[i], a[4 + i]);
+  *(void**)&f_attn = p[4];
+  *(void**)&f_gn = p[5];
+  *(void**)&f_gn_daq = p[6];
+  PyObject** keep[6] = {&g_get_device, &g_get_stream, &g_weight, &g_debug, &g_attn, &g_arg_error};
+  for (int i = 0; i < 6; ++i) {
+    Py_INCREF(a[7 + i]);
+    Py_XSETREF(*keep[i], a[7 + i]);
   }
   Py_RETURN_NONE;
 }
@@ -197,6 +271,9 @@ static PyMethodDef methods[] = {{"bind", FAST(bind)},
                                 {"wq_linear_residual", FAST(wq_linear_residual)},
                                 {"daq_quantize", FAST(daq_quantize)},
                                 {"ln_modulate_daq", FAST(ln_modulate_daq)},
+                                {"attention", FAST(attention)},
+                                {"group_norm", FAST(group_norm)},
+                                {"group_norm_daq", FAST(group_norm_daq)},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

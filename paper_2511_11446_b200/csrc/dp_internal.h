@@ -46,6 +46,15 @@ int launch_unpack(const UnpackJob& job, cudaStream_t stream, bool pdl);
 int launch_ln_modulate_daq(const void* x, int64_t M, int64_t K, int64_t ldx, const void* shift, const void* scale,
                            int64_t rows_per_sample, float eps, int8_t* q, int64_t ldq, float* s_a,
                            cudaStream_t stream, bool pdl);
+// norm.cu -- group normalisation + activation of channels-last maps, to bf16 (y) or to codes (q, s_a)
+int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, int64_t ldx, int32_t G, const void* gamma,
+                      const void* beta, float eps, bool silu, void* y, int64_t ldy, int8_t* q, int64_t ldq, float* s_a,
+                      void* workspace, cudaStream_t stream);
+size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t G);
+// attn.cu -- attention, mma.sync tiles of 16 queries
+struct AttnParams;
+int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl);
+int attn_init_device();
 int launch_daq_robust(const void* x, int64_t M, int64_t K, int64_t ldx, int8_t* q, int64_t ldq, float* s_a,
                       int32_t* rowsum, int clip_rank, int act_bits, bool tiled, cudaStream_t stream, bool pdl,
                       const UnpackJob* unpack);
