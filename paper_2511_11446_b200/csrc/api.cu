@@ -644,12 +644,15 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   p.max_q = static_cast<int32_t>(a->max_q), p.max_k = static_cast<int32_t>(a->max_k);
   p.q_start = a->q_start, p.k_start = a->k_start, p.prefix = a->prefix, p.slopes = a->slopes;
   const double log2e = 1.4426950408889634074;
-  p.scale = static_cast<float>(a->scale * log2e);
+  p.scale = fmaxf(static_cast<float>(a->scale * log2e), 1.2e-38f);  // (of a hidden score, -inf, also where scale is 0)
   p.cap = static_cast<float>(a->cap * log2e);
   p.scale_by_cap = a->cap != 0.0f ? static_cast<float>(2.0 * log2e * a->scale / a->cap) : 0.0f;
   p.causal = a->mask == DP_MASK_CAUSAL;
   p.status = device_status;
-  return launch_attn_rows(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));
+  const bool few = a->max_q * (H / KV) <= 64;
+  if (Mk == 0 || (flags & DP_FLAG_FORCE_SIMT) || (few && !(flags & DP_FLAG_FORCE_MMA)))
+    return launch_attn_rows(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));
+  return launch_attn_tc(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));
 }
 
 // ---- group normalisation ------------------------------------------------------------------------------

@@ -55,6 +55,11 @@ size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t G);
 struct AttnParams;
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl);
 int attn_init_device();
+// attn_tc.cu -- attention, tcgen05 tiles of 128 queries
+int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl);
+int attn_tc_init_device();
+int gemm_encode_heads(CUtensorMap* out, const void* base, int32_t D, int32_t heads, int64_t rows, int64_t hs, int64_t ld,
+                      uint32_t box_rows);
 int launch_daq_robust(const void* x, int64_t M, int64_t K, int64_t ldx, int8_t* q, int64_t ldq, float* s_a,
                       int32_t* rowsum, int clip_rank, int act_bits, bool tiled, cudaStream_t stream, bool pdl,
                       const UnpackJob* unpack);

@@ -415,6 +415,8 @@ int gemm_init_device(int dev, int* num_sms_out, int* max_pairs_out, int* max_clu
   if (st != DP_OK) return st;
   st = attn_init_device();
   if (st != DP_OK) return st;
+  st = attn_tc_init_device();
+  if (st != DP_OK) return st;
   *num_sms_out = sms;
   *max_pairs_out = pairs;
   return DP_OK;
@@ -457,6 +459,21 @@ int gemm_encode_w_rows(CUtensorMap* out, const void* base, uint64_t row_bytes, u
 int gemm_encode_bytes_2d(CUtensorMap* out, const void* base, uint64_t inner_bytes, uint64_t rows, uint64_t pitch_bytes,
                          uint32_t box_inner, uint32_t box_rows) {
   return encode_2d(out, base, inner_bytes, rows, pitch_bytes, box_inner, box_rows, true);
+}
+
+// bf16 vectors of D elements, `heads` of them hs elements apart in each of `rows` rows ld elements apart: boxes of 64 columns (zeros
+// behind D) of one head in box_rows rows, 128-byte swizzle.
+int gemm_encode_heads(CUtensorMap* out, const void* base, int32_t D, int32_t heads, int64_t rows, int64_t hs, int64_t ld,
+                      uint32_t box_rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(hs) * 2, static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[3] = {64, 1, box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = g_encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(DP_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  return DP_OK;
 }
 
 int gemm_encode_a(CUtensorMap* out, const int8_t* q, int64_t M, int64_t K, int64_t ldq) {
