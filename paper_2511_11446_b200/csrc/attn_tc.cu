@@ -1,17 +1,22 @@
 // Attention on the tensor cores: tcgen05 products with scores, weights and sums in tensor memory.
 //
-//   S = Q K^T (128 queries x 128 keys, fp32), t = scale S (capped, biased, masked), P = 2^(t - m) rounded to bf16 in place of S,
+//   S = Q K^T (128 queries x BN keys, fp32), t = scale S (capped, biased, masked), P = 2^(t - m) rounded to bf16,
 //   O += P V;  m: the row's running maximum, l: the row's running sum of the unrounded weights;  y = O / l
 //
 // One persistent CTA per SM takes work items of up to 256 queries of one head: two tiles of 128, each with a warpgroup whose
-// thread owns a row (no shuffles), so that one warpgroup's exponentials run beside the other's products. Warp 8 loads: Q once
-// an item, K and V tiles through one ring of TMA stages (128-byte swizzle, columns beyond head_dim zero-filled by the tensor
-// map); warp 9 issues the products, A of the second one (P) from tensor memory, V read along its rows as an MN-major operand.
-// Tensor memory: S0 S1 (128 columns each, P in the first 64 of them), O0 O1 (128 each).
+// thread owns a row (no shuffles) and with a thread that issues its products, so that one tile's exponentials run beside the
+// other's products. Warp 8 loads: Q once an item, K and V tiles through one ring of TMA stages that both tiles read (128-byte
+// swizzle, columns beyond head_dim zero-filled by the tensor map); A of the second product (P) comes from tensor memory, V is read
+// along its rows as an MN-major operand.
+// Tensor memory, 512 columns: S0 S1, P0 P1 (half as wide), O0 O1. With P beside S the next scores are computed while a warpgroup
+// still takes exponentials, which asks for 2 (3/2 BN + D) columns: 128 keys to a tile up to D = 64, 96 up to D = 96. Beyond, P lies
+// over S and the next scores wait for the product that reads it.
+//
+// A warp beside them decodes the work items ahead of everybody (a dozen divisions and the sequences' offsets), through a small
+// ring in shared memory.
 //
 // The maximum that the weights refer to moves only when a row's own maximum has outgrown it by 2^8: until then the sums stay
-// as they are (fp32 and bf16 have the range), and O is rescaled a few times an item instead of once a tile. A rescale needs no
-// barrier of its own: the products run in issue order, so S of a tile being there says that the product before it has ended.
+// as they are (fp32 and bf16 have the range), and O is rescaled a few times an item instead of once a tile.
 //
 // A tile that reaches behind the sequence's keys holds other sequences' rows, or nobody's: their scores are masked whatever they
 // are, and their V rows are overwritten with zeros before the product, since 0 * NaN would be NaN.
@@ -23,11 +28,30 @@
 
 namespace dp {
 
-constexpr int kTcTile = 128;                      // queries and keys of a tile
+constexpr int kTcTile = 128;                      // queries of a tile
 constexpr int kTcBlock = kTcTile * 128;           // bytes of 128 rows x 64 columns
-constexpr int kTcThreads = 320;
+constexpr int kTcThreads = 384;                   // two warpgroups; loads, an issuing warp for each tile, one idle
+// Registers a thread: 384 threads are launched with 168; the third warpgroup gives up what the first two take on:
+// 2 * 128 * 208 + 128 * 88 = 384 * 168.
+constexpr int kTcRegsLaunch = 168, kTcRegsSoftmax = 208, kTcRegsRest = 88;
+static_assert(256 * kTcRegsSoftmax + 128 * kTcRegsRest == kTcThreads * kTcRegsLaunch, "register split");
 constexpr float kTcRise = 8.0f;                   // log2 units by which a row's maximum may outgrow the reference
-__host__ __device__ constexpr int tc_stages(int nblk) { return nblk == 1 ? 8 : 5; }
+
+// Tiles for vectors of up to 16 KS elements.
+template <int KS>
+struct TcForm {
+  static constexpr bool kBeside = KS <= 6;                       // P has columns of its own
+  static constexpr int BN = KS <= 4 ? 128 : KS <= 6 ? 96 : 128;  // keys of a tile
+  static constexpr int D = 16 * KS, NBLK = (D + 63) / 64;
+  static constexpr int kQBytes = NBLK * kTcBlock, kKvBlock = BN * 128, kKvBytes = NBLK * kKvBlock;
+  static constexpr int NS = NBLK == 1 ? 8 : BN == 96 ? 6 : 4;    // ring stages
+  static constexpr uint32_t kS = 0, kP = kBeside ? 2 * BN : 0, kPStep = kBeside ? BN / 2 : BN;
+  static constexpr uint32_t kO = kBeside ? 3 * BN : 2 * BN;      // columns
+  static_assert(kO + 2 * D <= 512, "tensor memory");
+  // (after the tiles: the ring of items, barriers, turns, tensor memory's address, the abort flag)
+  static constexpr size_t kSmem = 1024 + 2 * kQBytes + NS * kKvBytes + 4 * 48 + (2 * NS + 12 + 2 * 4) * 8 + 48;
+  static_assert(kSmem <= 232448, "shared memory");
+};
 
 struct AttnTcSched {
   int32_t rows;        // queries of a work item: 128 or 256
@@ -89,17 +113,124 @@ __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t 
 }
 constexpr uint32_t kIdescBMn = 1u << 16;  // instruction descriptor: B is MN-major
 
+// The weights 2^(s scale - sub) of N scores, their sum and their bf16 pairs. The special-function unit takes 16 values a clock and SM,
+// for 96 scores of two warps to an SM quarter 1536 clocks of the 1640 that this takes. (A share of the powers by a cubic on the FMA
+// pipe, measured: 1360 clocks at two of eight pairs; in the kernel, where the warps take turns, nothing.)
+template <int N>
+__device__ __forceinline__ float tc_weights(const float (&s)[N], float scale, float sub, uint32_t (&w)[N / 2]) {
+  const uint64_t scale2 = f32x2_pack(scale, scale), sub2 = f32x2_pack(-sub, -sub);
+  uint64_t sum[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    float lo, hi;
+    f32x2_unpack(f32x2_fma(f32x2_pack(s[2 * i], s[2 * i + 1]), scale2, sub2), lo, hi);
+    lo = ex2(lo);
+    hi = ex2(hi);
+    sum[i & 1] = f32x2_add(sum[i & 1], f32x2_pack(lo, hi));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(hi), "f"(lo));
+  }
+  float u, v;
+  f32x2_unpack(f32x2_add(sum[0], sum[1]), u, v);
+  return u + v;
+}
+
+// tanh(s k) in place of N scores. As long as a warp's rows stay within 3/4, which capped scores of real models do, by an odd
+// polynomial fitted for the least relative error (7.2e-7), without the special-function unit; else two operations of it each.
+template <int N>
+__device__ __forceinline__ void tc_tanh(float (&s)[N], float two_log2e_k, float k) {
+  float top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < N; i += 2) top[(i >> 1) & 3] = fmaxf(fmaxf(top[(i >> 1) & 3], fabsf(s[i])), fabsf(s[i + 1]));
+  const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * k;
+  if (__all_sync(0xFFFFFFFFu, big <= 0.75f)) {
+    const uint64_t k2 = f32x2_pack(k, k);
+    const uint64_t c3 = f32x2_pack(0.01310583670f, 0.01310583670f), c2 = f32x2_pack(-0.05027795583f, -0.05027795583f);
+    const uint64_t c1 = f32x2_pack(0.13268236816f, 0.13268236816f), c0 = f32x2_pack(-0.33329668641f, -0.33329668641f);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint64_t u = f32x2_mul(f32x2_pack(s[i], s[i + 1]), k2), z = f32x2_mul(u, u);
+      uint64_t y = f32x2_fma(z, c3, c2);
+      y = f32x2_fma(y, z, c1);
+      y = f32x2_fma(y, z, c0);
+      f32x2_unpack(f32x2_fma(f32x2_mul(y, z), u, u), s[i], s[i + 1]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = capped(1.0f, s[i] * two_log2e_k);
+  }
+}
+
+// s scale - slope |pos - key| for N keys from key0 on; d = pos - key0, `side`: +1 if no key that counts lies behind pos, -1 if none
+// lies before it, 0 otherwise (the same for the whole warp).
+template <int N>
+__device__ __forceinline__ void tc_bias(float (&s)[N], float scale, float slope, int d, int side) {
+  if (side != 0) {
+    const float a = side > 0 ? slope : -slope, base = -a * static_cast<float>(d);  // + a (key - pos)
+    const uint64_t scale2 = f32x2_pack(scale, scale), step2 = f32x2_pack(2.0f * a, 2.0f * a);
+#pragma unroll
+    for (int g = 0; g < N; g += 16) {
+      const float first = fmaf(a, static_cast<float>(g), base);
+      uint64_t y = f32x2_pack(first, first + a);
+#pragma unroll
+      for (int i = g; i < g + 16; i += 2) {
+        f32x2_unpack(f32x2_fma(f32x2_pack(s[i], s[i + 1]), scale2, y), s[i], s[i + 1]);
+        y = f32x2_add(y, step2);
+      }
+    }
+  } else {
+    const float d0 = static_cast<float>(d);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = fmaf(-slope, fabsf(d0 - i), s[i] * scale);
+  }
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// 32 rows (one a lane) x 32 bf16 columns from registers to memory: lanes change their 16-byte pieces in fours, so that a store
+// writes 64 bytes of eight rows instead of 16 bytes of 32. row0: the warp's first row, of `live` ones.
+__device__ __forceinline__ void tc_store_32(uint16_t* y, int64_t ld, int row0, int live, int cols, const uint32_t (&w)[16]) {
+  const int lane = threadIdx.x & 31;
+  uint32_t e[4][4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[c][i] = w[4 * c + i];
+#pragma unroll
+  for (int b = 1; b <= 2; b <<= 1)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (c & b) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // the lane without the bit gives its piece c | b for the other's piece c
+        const bool up = lane & b;
+        const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, up ? e[c][i] : e[c | b][i], b);
+        if (up) e[c][i] = got;
+        else e[c | b][i] = got;
+      }
+    }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int row = row0 + (lane & 28) + k;
+    if (row < live && (lane & 3) * 8 < cols) st_global_v4(y + row * ld + (lane & 3) * 8, e[k]);
+  }
+}
+
 // A work item: the sequence, its queries' first row in it, and the key tiles that either tile of queries has to see.
-struct TcItem {
+struct __align__(16) TcItem {
   AttnSeq s;
-  int head, kvh, row0;
-  int n[2];  // key tiles of the two tiles of queries
-  int live[2];  // queries in them
-  bool valid;
-  __device__ __forceinline__ int tiles() const { return max(n[0], n[1]); }
+  int head, row0;    // row0 < 0: no more items
+  int n0, n1;        // key tiles of the two tiles of queries
+  int live0, live1;  // queries in them
+  __device__ __forceinline__ int n() const { return max(n0, n1); }
 };
-__device__ __forceinline__ TcItem tc_item(const AttnParams& p, const AttnTcSched& c, int item) {
-  TcItem r;
+constexpr int kTcSlots = 4;      // of the ring of items
+constexpr int kTcItemReaders = 11;  // loads, two issuing threads, eight warps
+template <int BN>
+__device__ __forceinline__ bool tc_item(const AttnParams& p, const AttnTcSched& c, int item, TcItem& r) {
   // pairs in groups; within a group the last rows, which see the most keys under a causal mask, come first
   const int pairs = p.H * p.n_seq;
   const int g = item / (c.group * c.tiles), in = item - g * c.group * c.tiles;
@@ -107,65 +238,71 @@ __device__ __forceinline__ TcItem tc_item(const AttnParams& p, const AttnTcSched
   const int tile = c.tiles - 1 - in / size, pair = g * c.group + in % size;
   const int seq = pair / p.H;
   r.head = pair - seq * p.H;
-  r.kvh = r.head / (p.H / p.KV);
   r.s = attn_seq(p, seq);
   r.row0 = tile * c.rows;
-  r.valid = r.row0 < r.s.nq;
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int first = r.row0 + t * kTcTile;
-    r.live[t] = t * kTcTile < c.rows ? min(max(r.s.nq - first, 0), kTcTile) : 0;
-    r.n[t] = r.live[t] > 0 ? (attn_keys(p, r.s, first + r.live[t] - 1) + kTcTile - 1) / kTcTile : 0;
-  }
-  return r;
+  if (r.row0 >= r.s.nq) return false;
+  r.live0 = min(r.s.nq - r.row0, kTcTile);
+  r.live1 = c.rows > kTcTile ? min(max(r.s.nq - r.row0 - kTcTile, 0), kTcTile) : 0;
+  r.n0 = (attn_keys(p, r.s, r.row0 + r.live0 - 1) + BN - 1) / BN;
+  r.n1 = r.live1 > 0 ? (attn_keys(p, r.s, r.row0 + kTcTile + r.live1 - 1) + BN - 1) / BN : 0;
+  return true;
 }
-// The i-th item of this CTA: rounds of gridDim.x items, every other one backwards, so that the long items that come first
+// The next item of this CTA: rounds of gridDim.x items, every other one backwards, so that the long items that come first
 // even out. False: there is none.
+template <int BN>
 __device__ __forceinline__ bool tc_next(const AttnParams& p, const AttnTcSched& c, int& round, TcItem& it) {
-  for (;; ++round) {
+  for (;;) {
     const int64_t base = static_cast<int64_t>(round) * gridDim.x;
     if (base >= c.items) return false;
     const int64_t i = base + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    if (i >= c.items) continue;
-    it = tc_item(p, c, static_cast<int>(i));
-    if (it.valid) {
-      ++round;
-      return true;
-    }
+    ++round;
+    if (i < c.items && tc_item<BN>(p, c, static_cast<int>(i), it)) return true;
   }
 }
 
-template <bool CAP, bool BIAS>
+template <int KS, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
-               const __grid_constant__ CUtensorMap tv, const AttnParams p, const AttnTcSched c, const int nblk) {
+               const __grid_constant__ CUtensorMap tv, const AttnParams p, const AttnTcSched c) {
+  using F = TcForm<KS>;
+  constexpr int BN = F::BN, NS = F::NS, NBLK = F::NBLK;
   extern __shared__ uint8_t smem_raw[];
-  const int NS = tc_stages(nblk), tile_bytes = nblk * kTcBlock;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* sQ = smem;                   // [2][nblk][128 rows][128 bytes]
-  uint8_t* sKV = sQ + 2 * tile_bytes;   // [NS][nblk][128 rows][128 bytes]
-  uint64_t* full = reinterpret_cast<uint64_t*>(sKV + NS * tile_bytes);
+  uint8_t* sQ = smem;                    // [2][NBLK][128 rows][128 bytes]
+  uint8_t* sKV = sQ + 2 * F::kQBytes;    // [NS][NBLK][BN rows][128 bytes]
+  TcItem* slots = reinterpret_cast<TcItem*>(sKV + NS * F::kKvBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(slots + kTcSlots);
   uint64_t* empty = full + NS;
-  uint64_t* q_full = empty + NS;
-  uint64_t* q_empty = q_full + 1;
-  uint64_t* s_full = q_empty + 1;  // [2]
-  uint64_t* p_full = s_full + 2;   // [2]
-  uint64_t* o_full = p_full + 2;   // [2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  uint64_t* item_full = empty + NS;
+  uint64_t* item_empty = item_full + kTcSlots;
+  uint64_t* q_full = item_empty + kTcSlots;  // [2]
+  uint64_t* q_empty = q_full + 2;            // [2]
+  uint64_t* s_full = q_empty + 2;  // [2] scores are there
+  uint64_t* s_read = s_full + 2;   // [2] and in the warpgroup's registers (P beside S only)
+  uint64_t* p_full = s_read + 2;   // [2] weights are there
+  uint64_t* pv_done = p_full + 2;  // [2] and their product has ended
+  volatile uint32_t* turns = reinterpret_cast<uint32_t*>(pv_done + 2);  // [8] tiles whose exponentials a warp has taken
+  uint32_t* tmem_slot = const_cast<uint32_t*>(turns) + 8;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NS; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&empty[i], 1);
+      mbar_init(&empty[i], 2);
     }
-    mbar_init(q_full, 1);
-    mbar_init(q_empty, 1);
+    for (int i = 0; i < kTcSlots; ++i) {
+      mbar_init(&item_full[i], 1);
+      mbar_init(&item_empty[i], kTcItemReaders);
+    }
+    for (int i = 0; i < 8; ++i) turns[i] = 0;
     for (int t = 0; t < 2; ++t) {
+      mbar_init(&q_full[t], 1);
+      mbar_init(&q_empty[t], 1);
       mbar_init(&s_full[t], 1);
+      mbar_init(&s_read[t], 4);
       mbar_init(&p_full[t], 4);
-      mbar_init(&o_full[t], 1);
+      mbar_init(&pv_done[t], 1);
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -173,7 +310,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
     tma_prefetch_desc(&tk);
     tma_prefetch_desc(&tv);
   }
-  if (warp == 9) {
+  if (warp == 8) {
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
@@ -184,229 +321,248 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
   pdl_wait();
   pdl_launch_dependents();
 
-  if (warp == 8) {
-    if (elect_one()) {
+  // The next item from the ring; `leader`: the thread that gives the slot back once all that read it with this one have.
+  Ring item_at;
+  auto next_item = [&](TcItem& it, bool warp_wide) {
+    bool ok = mbar_wait(&item_full[item_at.s], item_at.ph, abort_flag);
+    if (warp_wide) ok = __all_sync(0xFFFFFFFFu, ok);
+    if (!ok) {
+      it.row0 = -1;
+      return false;
+    }
+    it = slots[item_at.s];
+    if (warp_wide) __syncwarp();
+    if (!warp_wide || lane == 0) mbar_arrive(&item_empty[item_at.s]);
+    item_at.next(kTcSlots);
+    return true;
+  };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsRest));
+    if (warp == 8 && elect_one()) {
       // ================= loads =================
       Ring st;
       bool ok = true;
-      int round = 0, n_items = 0;
+      uint32_t items[2] = {0, 0};
       TcItem it;
-      auto load = [&](const CUtensorMap* map, int head, int row) {
-        if (!(ok = mbar_spin_wait(&empty[st.s], st.ph ^ 1u, abort_flag))) return;
-        mbar_arrive_expect_tx(&full[st.s], tile_bytes);
-        for (int b = 0; b < nblk; ++b)
-          tma_load_3d(smem_u32(sKV) + st.s * tile_bytes + b * kTcBlock, map, b * 64, head, row, &full[st.s]);
-        st.next(NS);
+      const uint32_t group = p.H / p.KV;
+      auto load_q = [&](int t) {
+        if (!(ok = mbar_wait(&q_empty[t], (items[t] & 1) ^ 1u, abort_flag))) return;
+        ++items[t];
+        mbar_arrive_expect_tx(&q_full[t], F::kQBytes);
+#pragma unroll
+        for (int b = 0; b < NBLK; ++b)
+          tma_load_3d(smem_u32(sQ) + t * F::kQBytes + b * kTcBlock, &tq, b * 64, it.head, it.s.q0 + it.row0 + t * kTcTile, &q_full[t]);
       };
-      while (ok && tc_next(p, c, round, it)) {
-        const int n = it.tiles();
-        if (n == 0) continue;
-        if (!(ok = mbar_spin_wait(q_empty, (n_items & 1) ^ 1u, abort_flag))) break;
-        const int q_tiles = it.n[1] > 0 ? 2 : 1;
-        mbar_arrive_expect_tx(q_full, q_tiles * tile_bytes);
-        for (int t = 0; t < q_tiles; ++t)
-          for (int b = 0; b < nblk; ++b)
-            tma_load_3d(smem_u32(sQ) + t * tile_bytes + b * kTcBlock, &tq, b * 64, it.head, it.s.q0 + it.row0 + t * kTcTile, q_full);
-        ++n_items;
-        for (int j = 0; j < n && ok; ++j) {
-          load(&tk, it.kvh, it.s.k0 + j * kTcTile);
-          if (ok) load(&tv, it.kvh, it.s.k0 + j * kTcTile);
+      while (ok && (ok = next_item(it, false)) && it.row0 >= 0) {
+        const int n = it.n();
+        if (it.n0 > 0) load_q(0);
+        const int kvh = it.head / group;
+        for (int j = 0; j < 2 * n && ok; ++j) {  // K, V, K, V, ..
+          if (!(ok = mbar_wait(&empty[st.s], st.ph ^ 1u, abort_flag))) break;
+          mbar_arrive_expect_tx(&full[st.s], F::kKvBytes);
+#pragma unroll
+          for (int b = 0; b < NBLK; ++b)
+            tma_load_3d(smem_u32(sKV) + st.s * F::kKvBytes + b * F::kKvBlock, (j & 1) ? &tv : &tk, b * 64, kvh,
+                        it.s.k0 + (j >> 1) * BN, &full[st.s]);
+          st.next(NS);
+          if (j == 0 && it.n1 > 0) load_q(1);
         }
       }
       if (!ok) producer_drain();
-    }
-  } else if (warp == 9) {
-    if (elect_one()) {
-      // ================= products =================
-      const int ks = (p.D + 15) / 16;
-      const uint32_t idesc_s = idesc_bf16(kTcTile, kTcTile), idesc_o = idesc_bf16(kTcTile, ks * 16) | kIdescBMn;
-      const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ)), k_desc = smem_desc_sw128(smem_u32(sKV));
-      const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sKV), kTcBlock);
-      Ring st;  // the next tile of the ring to be used
-      bool ok = true;
-      int round = 0, n_items = 0;
-      uint32_t p_ph[2] = {0, 0};
-      TcItem cur, nxt;
-      auto scores = [&](int t, int stage) {
-#pragma unroll 1
-        for (int k = 0; k < ks; ++k) {
-          const uint64_t at = static_cast<uint64_t>((k >> 2) * (kTcBlock >> 4) + (k & 3) * 2);
-          mma_bf16_ss(tmem + t * 128, q_desc + static_cast<uint64_t>(t * (tile_bytes >> 4)) + at,
-                      k_desc + static_cast<uint64_t>(stage * (tile_bytes >> 4)) + at, idesc_s, k != 0);
-        }
-        mma_commit(&s_full[t]);
-      };
-      // first scores of an item, for tile t; K's stage is st
-      bool have = tc_next(p, c, round, nxt);
-      bool first_in = false;  // nxt's Q and first K are there
-      auto enter = [&]() {    // waits for nxt's Q and first K tile
-        if (first_in) return true;
-        ok = mbar_spin_wait(q_full, n_items & 1, abort_flag) && mbar_spin_wait(&full[st.s], st.ph, abort_flag);
+    } else if (warp == 11 && elect_one()) {
+      // ================= work items =================
+      int round = 0;
+      TcItem it;
+      bool ok = true, more = true;
+      while (ok && more) {
+        more = tc_next<BN>(p, c, round, it);
+        if (!more) it.row0 = -1;
+        if (!(ok = mbar_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag))) break;
+        slots[item_at.s] = it;
+        mbar_arrive(&item_full[item_at.s]);
+        item_at.next(kTcSlots);
+      }
+    } else if ((warp == 9 || warp == 10) && elect_one()) {
+      // ================= products of tile t =================
+      const int t = warp - 9;
+      constexpr uint32_t idesc_s = idesc_bf16(kTcTile, BN), idesc_o = idesc_bf16(kTcTile, F::D) | kIdescBMn;
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ) + t * F::kQBytes), k_desc = smem_desc_sw128(smem_u32(sKV));
+      const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sKV), F::kKvBlock);
+      const uint32_t d_s = tmem + F::kS + t * BN, d_p = tmem + F::kP + t * F::kPStep, d_o = tmem + F::kO + t * F::D;
+      bool ok = true, ahead = false;  // ahead: the next item's first scores are issued
+      uint32_t n_s = 0, n_p = 0, items = 0;  // scores, weights, items so far
+      // Scores of the key tile in stage k into S, which the warpgroup has read.
+      auto scores = [&](const Ring& k) {
+        if (F::kBeside && n_s > 0 && !(ok = mbar_wait(&s_read[t], (n_s - 1) & 1, abort_flag))) return;
+        if (!(ok = mbar_wait(&full[k.s], k.ph, abort_flag))) return;
         tc_fence_after();
-        ++n_items;
-        first_in = true;
-        return ok;
+        const uint64_t kd = k_desc + static_cast<uint64_t>(k.s * (F::kKvBytes >> 4));
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+          mma_bf16_ss(d_s, q_desc + (i >> 2) * (kTcBlock >> 4) + (i & 3) * 2, kd + (i >> 2) * (F::kKvBlock >> 4) + (i & 3) * 2,
+                      idesc_s, i != 0);
+        mma_commit(&s_full[t]);
+        mma_commit(&empty[k.s]);
+        ++n_s;
       };
-      auto first_done = [&]() {  // both tiles' first scores are issued
-        mma_commit(&empty[st.s]);
-        st.next(NS);
-        if (nxt.tiles() == 1) mma_commit(q_empty);
+      auto first_scores = [&](const Ring& k, int n) {  // of an item with n key tiles for this tile
+        if (!(ok = mbar_wait(&q_full[t], items & 1, abort_flag))) return;
+        ++items;
+        scores(k);
+        if (ok && n == 1) mma_commit(&q_empty[t]);
       };
-      bool pending = have;  // nxt's first scores are still to be issued
-      while (ok && have) {
-        cur = nxt;
-        const int n = cur.tiles();
-        if (pending && n > 0) {
-          if (!enter()) break;
-          for (int t = 0; t < 2; ++t)
-            if (cur.n[t] > 0) scores(t, st.s);
-          first_done();
-        }
-        have = tc_next(p, c, round, nxt);
-        first_in = false;
-        pending = true;
-        for (int j = 0; j < n && ok; ++j) {
-          const Ring v = st;
-          st.next(NS);  // (the next K tile: of this item, or the next item's first)
-          const bool last = j + 1 == n;
-          const bool more = !last || (have && nxt.tiles() > 0);
-          bool v_in = false, k_in = false;
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (j < cur.n[t]) {
-              if (!(ok = mbar_spin_wait(&p_full[t], p_ph[t], abort_flag))) break;
-              p_ph[t] ^= 1u;
-              if (!v_in && !(ok = mbar_spin_wait(&full[v.s], v.ph, abort_flag))) break;
-              v_in = true;
-              tc_fence_after();
-#pragma unroll 1
-              for (int k = 0; k < kTcTile / 16; ++k)
-                mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + k * 8,
-                            v_desc + static_cast<uint64_t>(v.s * (tile_bytes >> 4) + k * 128), idesc_o, (j | k) != 0);
-              if (j + 1 == cur.n[t]) mma_commit(&o_full[t]);
-            }
-            if (t == 1) mma_commit(&empty[v.s]);
-            if (last) {  // the next item's first scores, while this one's last weights are under way
-              if (more && nxt.n[t] > 0) {
-                if (!enter()) break;
-                scores(t, st.s);
-              }
-            } else if (j + 1 < cur.n[t]) {
-              if (!k_in && !(ok = mbar_spin_wait(&full[st.s], st.ph, abort_flag))) break;
-              k_in = true;
-              tc_fence_after();
-              scores(t, st.s);
-            }
-          }
-          if (!ok) break;
-          if (last) {
-            if (more) {
-              first_done();
-              pending = false;
-            }
-          } else {
-            mma_commit(&empty[st.s]);
+      Ring st;  // K of the item's first tile
+      TcItem nxt;
+      ok = next_item(nxt, false);
+      while (ok && nxt.row0 >= 0) {
+        const int n_all = nxt.n(), n = t ? nxt.n1 : nxt.n0;
+        if (!(ok = next_item(nxt, false))) break;
+        const int n_next = nxt.row0 >= 0 ? (t ? nxt.n1 : nxt.n0) : 0;
+        if (n > 0) {
+          if (!ahead) first_scores(st, n);
+          ahead = false;
+          st.next(NS);
+          for (int j = 0; j < n && ok; ++j) {
+            const Ring v = st;
             st.next(NS);
-            if (j + 2 == n) mma_commit(q_empty);
+            auto next_scores = [&]() {
+              scores(st);
+              if (ok && j + 2 == n) mma_commit(&q_empty[t]);
+            };
+            if (F::kBeside && j + 1 < n) next_scores();
+            if (!ok || !(ok = mbar_wait(&p_full[t], n_p & 1, abort_flag)) || !(ok = mbar_wait(&full[v.s], v.ph, abort_flag))) break;
+            ++n_p;
+            tc_fence_after();
+            const uint64_t vd = v_desc + static_cast<uint64_t>(v.s * (F::kKvBytes >> 4));
+            const uint32_t add = j != 0;
+            mma_bf16_ts(d_o, d_p, vd, idesc_o, add);
+#pragma unroll
+            for (int i = 1; i < BN / 16; ++i) mma_bf16_ts(d_o, d_p + i * 8, vd + i * 128, idesc_o, 1u);
+            mma_commit(&pv_done[t]);
+            mma_commit(&empty[v.s]);
+            if (j + 1 < n) {
+              if (!F::kBeside) next_scores();
+              st.next(NS);
+            } else if (n == n_all && n_next > 0) {  // the next item's first scores while this one's output is written
+              first_scores(st, n_next);
+              ahead = true;
+            }
           }
+        }
+        // the rest of the item's tiles is the other tile's: passed on as they come
+        for (int j = 2 * n; j < 2 * n_all && ok; ++j) {
+          if (!(ok = mbar_wait(&full[st.s], st.ph, abort_flag))) break;
+          mbar_arrive(&empty[st.s]);
+          st.next(NS);
         }
       }
     }
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcRegsSoftmax));
     // ================= softmax: warpgroup t, thread <-> row =================
     const int t = warp >> 2;
     const int row = threadIdx.x & 127;
-    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + t * 128, to = tmem + lanes + 256 + t * 128;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const uint32_t a_s = lanes + F::kS + t * BN, a_p = lanes + F::kP + t * F::kPStep, a_o = lanes + F::kO + t * F::D;
     Ring st;
     bool ok = true;
-    int round = 0;
-    uint32_t s_ph = 0, o_ph = 0;
+    uint32_t n_s = 0, others = 0;  // tiles so far, the other warpgroup's up to this item
     TcItem it;
-    float s[128];
-    while (ok && tc_next(p, c, round, it)) {
-      const int n_all = it.tiles(), n = it.n[t];
-      const int q = it.row0 + t * kTcTile + row;  // this thread's query
-      const int pos = q + it.s.behind;
+    while (ok && (ok = next_item(it, true)) && it.row0 >= 0) {
+      const int n_all = it.n(), n = t ? it.n1 : it.n0, live = t ? it.live1 : it.live0;
+      const int pos = it.row0 + t * kTcTile + row + it.s.behind;  // of this thread's query
       // keys below this bound are visible
       const int bound = p.causal ? min(it.s.nk, max(pos + 1, it.s.prefix)) : it.s.nk;
       const float slope = BIAS ? ld_global_f32(p.slopes + it.head) * kLog2e : 0.0f;
-      const float scale = CAP || BIAS ? 1.0f : p.scale;
+      const float scale = BIAS ? 1.0f : CAP ? p.cap : p.scale;
       float m = -INFINITY, l = 0.0f;
       for (int j = 0; j < n_all; ++j) {
         st.next(NS);  // (K)
         const Ring v = st;
         st.next(NS);
         if (j >= n) continue;
-        ok = mbar_wait(&s_full[t], s_ph, abort_flag);
+        ok = mbar_wait(&s_full[t], n_s & 1, abort_flag);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        s_ph ^= 1u;
         tc_fence_after();
+        float s[BN];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld_x32(ts + i * 32, s + i * 32);
+        for (int i = 0; i < BN / 32; ++i) tmem_ld_x32(a_s + i * 32, s + i * 32);
         tmem_ld_wait();
-        const int left = bound - j * kTcTile;  // visible keys of this tile
-        if constexpr (CAP) {
-#pragma unroll
-          for (int i = 0; i < 128; ++i) s[i] = capped(p.cap, s[i] * p.scale_by_cap);
-        } else if constexpr (BIAS) {
-#pragma unroll
-          for (int i = 0; i < 128; ++i) s[i] *= p.scale;
+        if constexpr (F::kBeside) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&s_read[t]);
         }
+        const int left = bound - j * BN;  // visible keys of this tile
+        if constexpr (CAP) tc_tanh(s, p.scale_by_cap, p.scale_by_cap * (0.5f / kLog2e));
         if constexpr (BIAS) {
-          const float d0 = static_cast<float>(pos - j * kTcTile);
-#pragma unroll
-          for (int i = 0; i < 128; ++i) s[i] = fmaf(-slope, fabsf(d0 - i), s[i]);
+          const int d = pos - lane - j * BN;  // of the warp's first row
+          const int side = d >= BN - 1 || (p.causal && j * BN >= it.s.prefix) ? 1 : d + 31 <= 0 ? -1 : 0;
+          tc_bias(s, CAP ? p.cap : p.scale, slope, d + lane, side);
         }
-        if (__any_sync(0xFFFFFFFFu, left < kTcTile)) {
+        if (__any_sync(0xFFFFFFFFu, left < BN)) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i) s[i] = i < left ? s[i] : -INFINITY;
+          for (int g = 0; g < BN; g += 32)
+            if (__any_sync(0xFFFFFFFFu, left < g + 32)) {
+#pragma unroll
+              for (int i = g; i < g + 32; ++i) s[i] = i < left ? s[i] : -INFINITY;
+            }
         }
         float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int i = 4; i < 128; ++i) mx[i & 3] = fmaxf(mx[i & 3], s[i]);
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+        for (int i = 4; i < BN - 4; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], s[i], s[i + 1]);
+        const float top = fmaxf(max3(max3(mx[0], mx[1], s[BN - 4]), mx[2], s[BN - 3]), max3(mx[3], s[BN - 2], s[BN - 1])) * scale;
+        // P and O are this warpgroup's once the product before has ended
+        auto product_before = [&]() {
+          if (n_s == 0) return true;
+          ok = mbar_wait(&pv_done[t], (n_s - 1) & 1, abort_flag);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          tc_fence_after();
+          return ok;
+        };
         if (j == 0) {
           m = top;
         } else if (__any_sync(0xFFFFFFFFu, top > m + kTcRise)) {
+          if (!product_before()) break;
           const float to_m = fmaxf(m, top), f = to_m == -INFINITY ? 1.0f : ex2(m - to_m);
           m = to_m;
           l *= f;
 #pragma unroll 1
-          for (int k = 0; k < p.D; k += 16) {
+          for (int k = 0; k < F::D; k += 16) {
             float o[16];
-            tmem_ld_x16(to + k, o);
+            tmem_ld_x16(a_o + k, o);
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[i] *= f;
-            tmem_st_x16(to + k, reinterpret_cast<const uint32_t*>(o));
+            tmem_st_x16(a_o + k, reinterpret_cast<const uint32_t*>(o));
           }
         }
         const float sub = m == -INFINITY ? 0.0f : m;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float a = ex2(fmaf(s[k * 32 + 2 * i], scale, -sub)), b = ex2(fmaf(s[k * 32 + 2 * i + 1], scale, -sub));
-            sum[(2 * i) & 3] += a;
-            sum[(2 * i + 1) & 3] += b;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(b), "f"(a));
-          }
-          tmem_st_x16(ts + k * 16, w);
+        // The two warps of an SM quarter take turns at the exponentials: both at once would be no faster, and apart one's stand
+        // beside the other's loads, scans and waits (32 x 1024 tokens, 16 heads of 72: 250 us without turns, 237 with). A
+        // bounded wait: what it orders is time, not data.
+        const uint32_t until = others + min(j + t, t ? it.n0 : it.n1);
+        for (int i = 0; i < 64 && turns[warp ^ 4] < until; ++i) {
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        const int keys_here = it.s.nk - j * kTcTile;
-        if (keys_here < kTcTile) {  // V rows behind the sequence: zeros
+        uint32_t w[BN / 2];
+        l += tc_weights(s, scale, sub, w);
+        if (!(l < 0.0f)) turns[warp] = n_s + 1;  // (never negative: the store waits for the sum)
+        if (!product_before()) break;
+        ++n_s;
+#pragma unroll
+        for (int k = 0; k < BN / 32; ++k) tmem_st_x16(a_p + k * 16, w + k * 16);
+        const int keys_here = it.s.nk - j * BN;
+        if (keys_here < BN) {  // V rows behind the sequence: zeros
           ok = mbar_wait(&full[v.s], v.ph, abort_flag);
           ok = __all_sync(0xFFFFFFFFu, ok);
           if (!ok) break;
-          uint8_t* vt = sKV + v.s * tile_bytes + row * 128;
-          if (row >= keys_here)
-            for (int b = 0; b < nblk; ++b)
+          uint8_t* vt = sKV + v.s * F::kKvBytes + keys_here * 128;
 #pragma unroll
-              for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(vt + b * kTcBlock + i * 16) = make_uint4(0, 0, 0, 0);
+          for (int b = 0; b < NBLK; ++b)
+            for (int i = row; i < (BN - keys_here) * 8; i += 128)
+              *reinterpret_cast<uint4*>(vt + b * F::kKvBlock + i * 16) = make_uint4(0, 0, 0, 0);
           fence_proxy_async_smem();
         }
         tmem_st_wait();
@@ -415,45 +571,40 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         if (lane == 0) mbar_arrive(&p_full[t]);
       }
       if (!ok) break;
+      others += t ? it.n0 : it.n1;
+      if (live == 0) continue;
+      const float inv = l != 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;  // (no key in sight: O is zero too)
+      uint16_t* yt = p.y + static_cast<int64_t>(it.s.q0 + it.row0 + t * kTcTile) * p.ldy + it.head * p.y_hs;
+      float o[(F::D + 31) / 32 * 32];
       if (n > 0) {
-        ok = mbar_wait(&o_full[t], o_ph, abort_flag);
+        ok = mbar_wait(&pv_done[t], (n_s - 1) & 1, abort_flag);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        o_ph ^= 1u;
         tc_fence_after();
-      }
-      const bool live = row < it.live[t];
-      const float inv = l != 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;  // (no key in sight: O is zero too)
-      uint16_t* yr = p.y + static_cast<int64_t>(it.s.q0 + q) * p.ldy + it.head * p.y_hs;
-      if (it.live[t] > 0) {
-#pragma unroll 1
-        for (int k = 0; k < p.D; k += 16) {
-          float o[16];
-          if (n > 0) {
-            tmem_ld_x16(to + k, o);
-            tmem_ld_wait();
-          } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = 0.0f;
-          }
-          uint32_t w[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float a = o[2 * i] * inv, b = o[2 * i + 1] * inv;
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(b), "f"(a));
-          }
-          if (live) {
-            st_global_v4(yr + k, reinterpret_cast<const uint32_t(&)[4]>(w[0]));
-            if (k + 8 < p.D) st_global_v4(yr + k + 8, reinterpret_cast<const uint32_t(&)[4]>(w[4]));
-          }
-        }
+        for (int k = 0; k < F::D; k += 16) tmem_ld_x16(a_o + k, o + k);
+        tmem_ld_wait();
         tc_fence_before();  // (the next item's products write O behind this thread's next arrival on p_full)
+      } else {
+#pragma unroll
+        for (int k = 0; k < F::D; ++k) o[k] = 0.0f;
+      }
+#pragma unroll
+      for (int k = 0; k < F::D; k += 32) {
+        if (k >= p.D) break;
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float a = k + 2 * i < F::D ? o[k + 2 * i] * inv : 0.0f, b = k + 2 * i < F::D ? o[k + 2 * i + 1] * inv : 0.0f;
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(b), "f"(a));
+        }
+        tc_store_32(yt + k, p.ldy, (warp & 3) * 32, live, p.D - k, w);
       }
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == 8) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -461,30 +612,47 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
 }
 
 // ---- host side -------------------------------------------------------------------------------------
-static size_t tc_smem_bytes(int nblk) {
-  return 1024 + static_cast<size_t>(2 + tc_stages(nblk)) * nblk * kTcBlock + (2 * tc_stages(nblk) + 8) * 8 + 16;
-}
-template <bool CAP, bool BIAS>
+template <int KS, bool CAP, bool BIAS>
 static cudaError_t tc_init() {
-  const size_t a = tc_smem_bytes(1), b = tc_smem_bytes(2);
-  return cudaFuncSetAttribute(attn_tc_kernel<CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(a > b ? a : b));
+  return cudaFuncSetAttribute(attn_tc_kernel<KS, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(TcForm<KS>::kSmem));
+}
+template <int KS>
+static int tc_init_ks() {
+  DP_CUDA_OK((tc_init<KS, false, false>()));
+  DP_CUDA_OK((tc_init<KS, false, true>()));
+  DP_CUDA_OK((tc_init<KS, true, false>()));
+  DP_CUDA_OK((tc_init<KS, true, true>()));
+  return DP_OK;
 }
 int attn_tc_init_device() {
-  DP_CUDA_OK((tc_init<false, false>()));
-  DP_CUDA_OK((tc_init<false, true>()));
-  DP_CUDA_OK((tc_init<true, false>()));
-  DP_CUDA_OK((tc_init<true, true>()));
+  int st = tc_init_ks<4>();
+  if (st == DP_OK) st = tc_init_ks<5>();
+  if (st == DP_OK) st = tc_init_ks<6>();
+  if (st == DP_OK) st = tc_init_ks<8>();
+  return st;
+}
+
+template <int KS>
+static int launch_tc(const AttnParams& p, const AttnTcSched& c, unsigned ctas, cudaStream_t stream, bool pdl) {
+  using F = TcForm<KS>;
+  CUtensorMap tq, tk, tv;
+  int st = gemm_encode_heads(&tq, p.q, p.D, p.H, p.Mq, p.q_hs, p.ldq, kTcTile);
+  if (st == DP_OK) st = gemm_encode_heads(&tk, p.k, p.D, p.KV, p.Mk, p.k_hs, p.ldk, F::BN);
+  if (st == DP_OK) st = gemm_encode_heads(&tv, p.v, p.D, p.KV, p.Mk, p.v_hs, p.ldv, F::BN);
+  if (st != DP_OK) return st;
+  const dim3 grid(ctas), block(kTcThreads);
+  const bool cap = p.cap != 0.0f, bias = p.slopes != nullptr;
+  const cudaError_t e =
+      cap && bias ? launch(attn_tc_kernel<KS, true, true>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+      : cap       ? launch(attn_tc_kernel<KS, true, false>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+      : bias      ? launch(attn_tc_kernel<KS, false, true>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+                  : launch(attn_tc_kernel<KS, false, false>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c);
+  if (e != cudaSuccess) return fail(DP_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
   return DP_OK;
 }
 
 int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
-  const int nblk = (p.D + 63) / 64;
-  CUtensorMap tq, tk, tv;
-  int st = gemm_encode_heads(&tq, p.q, p.D, p.H, p.Mq, p.q_hs, p.ldq, kTcTile);
-  if (st == DP_OK) st = gemm_encode_heads(&tk, p.k, p.D, p.KV, p.Mk, p.k_hs, p.ldk, kTcTile);
-  if (st == DP_OK) st = gemm_encode_heads(&tv, p.v, p.D, p.KV, p.Mk, p.v_hs, p.ldv, kTcTile);
-  if (st != DP_OK) return st;
   const int sms = num_sms() > 0 ? num_sms() : 148;
   const int64_t pairs = static_cast<int64_t>(p.H) * p.n_seq;
   AttnTcSched c;
@@ -499,15 +667,11 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   // Without a mask all items are alike and a pair's stand together, for its K and V in L2; with one, 64 pairs.
   const int64_t group = p.causal ? 64 : 1;
   c.group = static_cast<int32_t>(group < pairs ? group : pairs);
-  const dim3 grid(static_cast<unsigned>(c.items < sms ? c.items : sms)), block(kTcThreads);
-  const size_t smem = tc_smem_bytes(nblk);
-  cudaError_t e;
-  if (p.cap != 0.0f && p.slopes != nullptr) e = launch(attn_tc_kernel<true, true>, grid, block, smem, stream, pdl, tq, tk, tv, p, c, nblk);
-  else if (p.cap != 0.0f) e = launch(attn_tc_kernel<true, false>, grid, block, smem, stream, pdl, tq, tk, tv, p, c, nblk);
-  else if (p.slopes != nullptr) e = launch(attn_tc_kernel<false, true>, grid, block, smem, stream, pdl, tq, tk, tv, p, c, nblk);
-  else e = launch(attn_tc_kernel<false, false>, grid, block, smem, stream, pdl, tq, tk, tv, p, c, nblk);
-  if (e != cudaSuccess) return fail(DP_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
-  return DP_OK;
+  const unsigned ctas = static_cast<unsigned>(c.items < sms ? c.items : sms);
+  return p.D <= 64   ? launch_tc<4>(p, c, ctas, stream, pdl)
+         : p.D <= 80 ? launch_tc<5>(p, c, ctas, stream, pdl)
+         : p.D <= 96 ? launch_tc<6>(p, c, ctas, stream, pdl)
+                     : launch_tc<8>(p, c, ctas, stream, pdl);
 }
 
 }  // namespace dp
