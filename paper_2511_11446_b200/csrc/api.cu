@@ -657,8 +657,7 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
 
 // ---- group normalisation ------------------------------------------------------------------------------
 extern "C" size_t dp_group_norm_workspace(int64_t n_samples, int64_t rows, int32_t C, int32_t groups) {
-  (void)C;
-  return group_norm_workspace(n_samples, rows, groups < 1 ? 1 : groups);
+  return group_norm_workspace(n_samples, rows, C, groups < 1 ? 1 : groups);
 }
 
 static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, int32_t C, int64_t ldx, int32_t G,
@@ -678,8 +677,8 @@ static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, 
   if (!aligned16(x) || !aligned16(out) || (ldx % 8) || (ldo * out_size % 16) || !aligned16(gamma) || !aligned16(beta) ||
       (reinterpret_cast<uintptr_t>(s_a) & 3u))
     return fail(DP_ERR_ALIGN, "%s: pointers and pitches must be 16-byte aligned", name);
-  if (!workspace || workspace_bytes < group_norm_workspace(n, rows, G) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
-    return fail(DP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, 256-byte aligned", name, group_norm_workspace(n, rows, G));
+  if (!workspace || workspace_bytes < group_norm_workspace(n, rows, C, G) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+    return fail(DP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, 256-byte aligned", name, group_norm_workspace(n, rows, C, G));
   if (ranges_meet(x, 2 * ((n * rows - 1) * ldx + C), out, out_size * ((n * rows - 1) * ldo + C)))
     return fail(DP_ERR_INVALID_ARG, "%s: the output overlaps x", name);
   int st = check_device();

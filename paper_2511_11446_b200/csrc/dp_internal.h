@@ -50,7 +50,8 @@ int launch_ln_modulate_daq(const void* x, int64_t M, int64_t K, int64_t ldx, con
 int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, int64_t ldx, int32_t G, const void* gamma,
                       const void* beta, float eps, bool silu, void* y, int64_t ldy, int8_t* q, int64_t ldq, float* s_a,
                       void* workspace, cudaStream_t stream);
-size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t G);
+size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t C, int32_t G);
+int group_norm_init_device();
 // attn.cu -- attention, mma.sync tiles of 16 queries
 struct AttnParams;
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl);

@@ -7,21 +7,31 @@
 // In front of a U-Net block's projections the paper's method quantizes the activations like any other linear's (Eq. "daq");
 // dp_group_norm_daq writes the codes in the pass that would write y.
 //
-// Statistics first, from one pass over x: sums of d and d^2, d = x - pivot with the group's first value as pivot, so that a
-// level far above the spread does not cancel (a constant map gives var = 0 and h = beta exactly). A thread keeps 8 channels
-// of every R-th row, sums in fp32 over at most a few thousand values, and a CTA leaves one pair of sums per group; the second
-// kernel adds the CTAs' sums in double, in a fixed order, and makes one coefficient pair per channel of them:
+// Statistics first: sums of d and d^2, d = x - pivot with the group's first value as pivot, so that a level far above the spread
+// does not cancel (a constant map gives var = 0 and h = beta exactly). A thread keeps 8 channels of every `lanes`-th row, in fp32
+// over at most a few thousand values; groups' sums of CTAs are added in double, in a fixed order, and give each channel
 //     h = (x - pivot) * a + b,   a = gamma * rstd,   b = beta - (mean - pivot) * a       (x - pivot is exact or nearly so)
+//
+// Bound by memory: 2 bytes in and 2 (or 1) out per element, if x need not be read twice from it. Two forms:
+//  - maps of up to 8 x 64 KB or so a sample: one kernel, a cluster of CTAs to a sample. Each keeps its rows in shared memory while the
+//    group sums meet through distributed shared memory; x is read once, and there is one launch.
+//  - larger ones: a kernel of sums and one that applies them, which reads x again: from the L2 as far as it is still there, the last
+//    rows first. (A few samples at a time, so that all of it is: 16 samples of 16384 x 320, 10 MB each, 140 us by two, 101 by four,
+//    103 by eight, 96 all at once: each pair of launches costs more than the second read.)
 #include "daq_device.cuh"
 
 namespace dp {
 
-constexpr int kGnThreads = 256, kGnMaxChunks = 128;
+constexpr int kGnMaxChunks = 128, kGnMaxThreads = 640;
+constexpr int kGnUnroll = 4;                   // rows that a thread adds while as many are in flight
+constexpr int kGnMaxCluster = 8;               // (16, measured: 8 samples of 64 x 640 12.7 us, 6.5 with 8)
+constexpr size_t kGnSmem = 113 * 1024;          // of a CTA: two to an SM, one of which reads while the other writes
 
 struct GnArgs {
   const uint16_t* x;
   int64_t rows, ldx;  // rows of a sample
-  int32_t C, G;
+  int32_t C, G, per;   // per: channels of a group
+  uint64_t per_inv;    // ceil(2^32 / per): c / per = c * per_inv >> 32 for c < 2^16 (a division takes twenty instructions)
   const uint16_t *gamma, *beta;  // [C] or null
   float eps;
   uint16_t* y;
@@ -30,30 +40,37 @@ struct GnArgs {
   int64_t ldq;
   float* s_a;
   float2* sums;  // [sample][chunk][G]
-  int32_t chunks;
+  int32_t chunks;      // (CTAs of the cluster in the one-kernel form)
   int64_t chunk_rows;
 };
 
-__device__ __forceinline__ float gn_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float gn_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float gn_bf16(const uint16_t* p) {
   uint16_t v;
   asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
   return __uint_as_float(static_cast<uint32_t>(v) << 16);
 }
-__device__ __forceinline__ void gn_unpack(const uint4& v, float (&f)[8]) {
+// Eight bf16 as four packed fp32 pairs.
+__device__ __forceinline__ void gn_unpack(const uint4& v, uint64_t (&f)[4]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    f[2 * j] = gn_lo(w[j]);
-    f[2 * j + 1] = gn_hi(w[j]);
-  }
+  for (int j = 0; j < 4; ++j) f[j] = static_cast<uint64_t>(w[j] & 0xFFFF0000u) << 32 | static_cast<uint32_t>(w[j] << 16);
 }
+// act of a pair. SiLU h / (1 + e^-h): the special-function unit would be the bound at two operations an element (2 x 16 bf16 bytes
+// take it as long as they take memory), so a pair shares a reciprocal: 1 / u = v / (uv). Powers end at 2^62, so that products
+// stay finite: from h = -43 on the result is h 2^-62 instead of less. Both operations are good to 2^-22.
 template <bool SILU>
-__device__ __forceinline__ float gn_act(float h) {
+__device__ __forceinline__ uint64_t gn_act(uint64_t h) {
   if constexpr (!SILU) return h;
-  return __fdividef(h, 1.0f + __expf(-h));
+  float lo, hi, u, v, r;
+  f32x2_unpack(f32x2_mul(h, f32x2_pack(-1.4426950408889634f, -1.4426950408889634f)), lo, hi);
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(u) : "f"(fminf(lo, 62.0f)));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(v) : "f"(fminf(hi, 62.0f)));
+  f32x2_unpack(f32x2_add(f32x2_pack(u, v), f32x2_pack(1.0f, 1.0f)), u, v);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(u * v));
+  return f32x2_mul(h, f32x2_mul(f32x2_pack(r, r), f32x2_pack(v, u)));
 }
+
+__device__ __forceinline__ int gn_group(const GnArgs& a, int c) { return static_cast<int>(c * a.per_inv >> 32); }
 
 // Threads of a CTA: `lanes` rows of C / 8 vectors at a time.
 struct GnThread {
@@ -66,233 +83,447 @@ struct GnThread {
   }
 };
 
-__global__ void gn_stats_kernel(const GnArgs a) {
-  extern __shared__ float gn_part[];  // [2][lanes][C]
-  pdl_launch_dependents();
-  const GnThread t(a.C);
-  const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  const int per = a.C / a.G;
-  const int64_t r0 = chunk * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
-  pdl_wait();
-  const uint16_t* xs = a.x + sample * a.rows * a.ldx;
-  float s[8], ss[8], pivot[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    s[j] = ss[j] = 0.0f;
-    pivot[j] = gn_bf16(xs + (t.vec * 8 + j) / per * per);
-  }
+// Sums of rows [r0, r1) of a sample (xs) by group into out[G] (shared memory or global); with KEEP the rows go to `rows_at` too.
+// part: [2][lanes][C] floats of shared memory.
+template <bool KEEP>
+__device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, const uint16_t* xs, int64_t r0, int64_t r1, float* part,
+                                        uint4* rows_at, float2* out) {
   if (t.lane < t.lanes) {
-    const uint16_t* xp = xs + t.vec * 8;
-    for (int64_t r = r0 + t.lane; r < r1; r += t.lanes) {
-      uint4 v;
-      ld_stream_u32x4(reinterpret_cast<const uint4*>(xp + r * a.ldx), v);
-      float f[8];
+    uint64_t s2[4], ss2[4], minus[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      s2[j] = ss2[j] = 0;
+      minus[j] = f32x2_pack(-gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j) * a.per), -gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j + 1) * a.per));
+    }
+    int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;  // rows of this thread
+    const uint16_t* xp = xs + (r0 + t.lane) * a.ldx + t.vec * 8;
+    uint4* keep = rows_at + t.lane * t.vecs + t.vec;
+    const int64_t step = t.lanes * a.ldx;
+    const int keep_step = t.lanes * t.vecs;
+    auto add = [&](const uint4& v) {
+      uint64_t f[4];
       gn_unpack(v, f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = f[j] - pivot[j];
-        s[j] += d;
-        ss[j] = fmaf(d, d, ss[j]);
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t d = f32x2_add(f[j], minus[j]);
+        s2[j] = f32x2_add(s2[j], d);
+        ss2[j] = f32x2_fma(d, d, ss2[j]);
       }
-    }
-    float* ps = gn_part + t.lane * a.C + t.vec * 8;
+    };
+    // the next rows are on their way while these are added
+    uint4 v[kGnUnroll];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      ps[j] = s[j];
-      ps[t.lanes * a.C + j] = ss[j];
+    for (int u = 0; u < kGnUnroll; ++u, xp += step)
+      if (u < n) v[u] = ld_global_v4(xp);
+    for (; n > 0; n -= kGnUnroll) {
+      uint4 nx[kGnUnroll];
+#pragma unroll
+      for (int u = 0; u < kGnUnroll; ++u, xp += step)
+        if (u + kGnUnroll < n) nx[u] = ld_global_v4(xp);
+#pragma unroll
+      for (int u = 0; u < kGnUnroll; ++u)
+        if (u < n) {
+          if constexpr (KEEP) keep[u * keep_step] = v[u];
+          add(v[u]);
+        }
+      if constexpr (KEEP) keep += kGnUnroll * keep_step;
+#pragma unroll
+      for (int u = 0; u < kGnUnroll; ++u) v[u] = nx[u];
     }
+    float s[8], ss[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x2_unpack(s2[j], s[2 * j], s[2 * j + 1]);
+      f32x2_unpack(ss2[j], ss[2 * j], ss[2 * j + 1]);
+    }
+    float4* ps = reinterpret_cast<float4*>(part + t.lane * a.C + t.vec * 8);
+    float4* pss = reinterpret_cast<float4*>(part + (t.lanes + t.lane) * a.C + t.vec * 8);
+    ps[0] = make_float4(s[0], s[1], s[2], s[3]);
+    ps[1] = make_float4(s[4], s[5], s[6], s[7]);
+    pss[0] = make_float4(ss[0], ss[1], ss[2], ss[3]);
+    pss[1] = make_float4(ss[4], ss[5], ss[6], ss[7]);
   }
   __syncthreads();
-  const int warp = threadIdx.x >> 5, ln = threadIdx.x & 31;
-  for (int g = warp; g < a.G; g += blockDim.x >> 5) {
+  // channel by channel over the lanes, in the first lane's place, then group by group
+  for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
     float u = 0.0f, w = 0.0f;
-    for (int i = ln; i < t.lanes * per; i += 32) {
-      const int at = i / per * a.C + g * per + i % per;
-      u += gn_part[at];
-      w += gn_part[t.lanes * a.C + at];
+    for (int l = 0; l < t.lanes; ++l) {
+      u += part[l * a.C + c];
+      w += part[(t.lanes + l) * a.C + c];
     }
+    part[c] = u;
+    part[t.lanes * a.C + c] = w;
+  }
+  __syncthreads();
+  const float *cu = part, *cw = part + t.lanes * a.C;
+  if (a.per <= 48) {  // a thread to a group
+    for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
+      float u = 0.0f, w = 0.0f;
+      for (int i = 0; i < a.per; ++i) {
+        u += cu[g * a.per + i];
+        w += cw[g * a.per + i];
+      }
+      out[g] = make_float2(u, w);
+    }
+  } else {  // a warp
+    const int warp = threadIdx.x >> 5, ln = threadIdx.x & 31;
+    for (int g = warp; g < a.G; g += blockDim.x >> 5) {
+      float u = 0.0f, w = 0.0f;
+      for (int i = ln; i < a.per; i += 32) {
+        u += cu[g * a.per + i];
+        w += cw[g * a.per + i];
+      }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
-      w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
+      for (int o = 16; o > 0; o >>= 1) {
+        u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
+        w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
+      }
+      if (ln == 0) out[g] = make_float2(u, w);
     }
-    if (ln == 0) a.sums[(static_cast<int64_t>(sample) * a.chunks + chunk) * a.G + g] = make_float2(u, w);
   }
 }
 
-// Per group: (pivot, mean - pivot, rstd) into shared memory, from all chunks' sums.
-__device__ __forceinline__ void gn_groups(const GnArgs& a, int sample, float* out) {
-  const int warp = threadIdx.x >> 5, ln = threadIdx.x & 31, per = a.C / a.G;
-  const uint16_t* xs = a.x + sample * a.rows * a.ldx;
-  for (int g = warp; g < a.G; g += blockDim.x >> 5) {
+// Per group (pivot, mean - pivot, rstd) in shared memory, from the sums of `parts` CTAs: fetch(part, group).
+template <typename Fetch>
+__device__ __forceinline__ void gn_groups(const GnArgs& a, const uint16_t* xs, int parts, float* out, Fetch fetch) {
+  // 2^k threads to a group
+  int sub = 1;
+  while (sub < 32 && 2 * sub * a.G <= static_cast<int>(blockDim.x) && sub < parts) sub *= 2;
+  const int step = blockDim.x / sub;
+  for (int g0 = 0; g0 < a.G; g0 += step) {  // (the same trips for all threads: shuffles)
+    const int g = g0 + threadIdx.x / sub, k = threadIdx.x % sub;
+    const bool live = g < a.G && static_cast<int>(threadIdx.x) < step * sub;
     double u = 0.0, w = 0.0;
-    for (int c = ln; c < a.chunks; c += 32) {
-      float2 v;
-      const float2* p = a.sums + (static_cast<int64_t>(sample) * a.chunks + c) * a.G + g;
-      asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
-      u += v.x;
-      w += v.y;
-    }
+    if (live)
+      for (int c = k; c < parts; c += 8 * sub) {
+        float2 v[8];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
+        for (int i = 0; i < 8; ++i) v[i] = c + i * sub < parts ? fetch(c + i * sub, g) : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          u += v[i].x;
+          w += v[i].y;
+        }
+      }
+    for (int o = sub >> 1; o > 0; o >>= 1) {
       u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
       w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
     }
-    if (ln == 0) {
-      const double n = static_cast<double>(a.rows) * per, mean = u / n;
+    if (live && k == 0) {
+      const double n = static_cast<double>(a.rows) * a.per, mean = u / n;
       const double var = fmax(w / n - mean * mean, 0.0);
-      out[3 * g] = gn_bf16(xs + g * per);
+      out[3 * g] = gn_bf16(xs + g * a.per);
       out[3 * g + 1] = static_cast<float>(mean);
       out[3 * g + 2] = static_cast<float>(1.0 / sqrt(var + static_cast<double>(a.eps)));
     }
   }
 }
-// Coefficients of 8 channels.
-__device__ __forceinline__ void gn_coefs(const GnArgs& a, const float* groups, int c0, float (&pv)[8], float (&ca)[8],
-                                         float (&cb)[8]) {
-  const int per = a.C / a.G;
+// Coefficients of 8 channels, in pairs; `minus`: the pivots' negatives.
+struct GnCoefs {
+  uint64_t minus[4], a[4], b[4];
+  __device__ __forceinline__ uint64_t h(uint64_t x, int j) const { return f32x2_fma(f32x2_add(x, minus[j]), a[j], b[j]); }
+};
+__device__ __forceinline__ void gn_coefs(const GnArgs& a, const float* groups, int c0, GnCoefs& k) {
+  uint64_t gm[4], bt[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float* g = groups + (c0 + j) / per * 3;
-    pv[j] = g[0];
-    ca[j] = (a.gamma != nullptr ? gn_bf16(a.gamma + c0 + j) : 1.0f) * g[2];
-    cb[j] = fmaf(-g[1], ca[j], a.beta != nullptr ? gn_bf16(a.beta + c0 + j) : 0.0f);
+  for (int j = 0; j < 4; ++j) {
+    gm[j] = f32x2_pack(1.0f, 1.0f);
+    bt[j] = 0;
+  }
+  if (a.gamma != nullptr) {
+    gn_unpack(ld_global_v4(a.gamma + c0), gm);
+    gn_unpack(ld_global_v4(a.beta + c0), bt);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float *g = groups + gn_group(a, c0 + 2 * j) * 3, *h = groups + gn_group(a, c0 + 2 * j + 1) * 3;
+    k.minus[j] = f32x2_pack(-g[0], -h[0]);
+    k.a[j] = f32x2_mul(gm[j], f32x2_pack(g[2], h[2]));
+    k.b[j] = f32x2_fma(f32x2_pack(-g[1], -h[1]), k.a[j], bt[j]);
   }
 }
 
-template <bool SILU>
-__global__ void gn_apply_kernel(const GnArgs a) {
-  extern __shared__ float gn_part[];  // [G][3]
-  pdl_launch_dependents();
-  const GnThread t(a.C);
-  const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  const int64_t r0 = chunk * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
-  pdl_wait();
-  gn_groups(a, sample, gn_part);
-  __syncthreads();
+// bf16 output of rows [r0, r1). Source: where a row's vectors are read, by next row of the thread.
+template <bool SILU, typename Source>
+__device__ __forceinline__ void gn_write(const GnArgs& a, const GnThread& t, const float* groups, int64_t m0, int64_t r0, int64_t r1,
+                                         Source src) {
   if (t.lane >= t.lanes) return;
-  float pv[8], ca[8], cb[8];
-  gn_coefs(a, gn_part, t.vec * 8, pv, ca, cb);
-  const uint16_t* xp = a.x + sample * a.rows * a.ldx + t.vec * 8;
-  uint16_t* yp = a.y + sample * a.rows * a.ldy + t.vec * 8;
-  for (int64_t r = r0 + t.lane; r < r1; r += t.lanes) {
-    const uint4 v = ld_global_v4(xp + r * a.ldx);
-    float f[8];
+  GnCoefs k;
+  gn_coefs(a, groups, t.vec * 8, k);
+  int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;
+  uint16_t* yp = a.y + (m0 + r0 + t.lane) * a.ldy + t.vec * 8;
+  const int64_t step = t.lanes * a.ldy;
+  src.start(r0 + t.lane, t.vec, t.lanes);
+  auto put = [&](const uint4& v) {
+    uint64_t f[4];
     gn_unpack(v, f);
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float h0 = gn_act<SILU>(fmaf(f[2 * j] - pv[2 * j], ca[2 * j], cb[2 * j]));
-      const float h1 = gn_act<SILU>(fmaf(f[2 * j + 1] - pv[2 * j + 1], ca[2 * j + 1], cb[2 * j + 1]));
-      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(h1), "f"(h0));
+      float lo, hi;
+      f32x2_unpack(gn_act<SILU>(k.h(f[j], j)), lo, hi);
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(hi), "f"(lo));
     }
-    st_global_v4(yp + r * a.ldy, w);
+    st_global_v4(yp, w);
+    yp += step;
+  };
+  uint4 v[kGnUnroll];
+#pragma unroll
+  for (int u = 0; u < kGnUnroll; ++u)
+    if (u < n) v[u] = src.next();
+  for (; n > 0; n -= kGnUnroll) {
+    uint4 nx[kGnUnroll];
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u)
+      if (u + kGnUnroll < n) nx[u] = src.next();
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u)
+      if (u < n) put(v[u]);
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u) v[u] = nx[u];
+  }
+}
+struct GnFromGlobal {
+  const uint16_t* x;  // the sample
+  int64_t ldx, step = 0;
+  const uint16_t* at = nullptr;
+  __device__ __forceinline__ void start(int64_t row, int vec, int rows) {
+    at = x + row * ldx + vec * 8;
+    step = rows * ldx;
+  }
+  __device__ __forceinline__ uint4 next() {
+    const uint4 v = ld_global_v4(at);
+    at += step;
+    return v;
+  }
+};
+struct GnFromShared {
+  const uint4* x;  // rows from r0 on
+  int64_t r0;
+  int vecs, step = 0;
+  const uint4* at = nullptr;
+  __device__ __forceinline__ void start(int64_t row, int vec, int rows) {
+    at = x + static_cast<int>(row - r0) * vecs + vec;
+    step = rows * vecs;
+  }
+  __device__ __forceinline__ uint4 next() {
+    const uint4 v = *at;
+    at += step;
+    return v;
+  }
+};
+
+// Codes of rows [r0, r1), kGnUnroll x lanes rows a turn: a thread's values of its rows stay in registers while the rows' maxima meet
+// in shared memory (warps first, then an atomic maximum each) and one thread a row makes scale and reciprocal of its. `scales`:
+// kGnUnroll x lanes pairs of (maximum, then reciprocal) words, zero before and after.
+template <bool SILU, typename Source>
+__device__ __forceinline__ void gn_codes(const GnArgs& a, const GnThread& t, const float* groups, uint32_t* scales, int64_t m0,
+                                         int64_t r0, int64_t r1, Source src) {
+  const bool live = t.lane < t.lanes;
+  const int rows = static_cast<int>(r1 - r0), turn = kGnUnroll * t.lanes;
+  GnCoefs k;
+  gn_coefs(a, groups, t.vec * 8, k);
+  src.start(r0 + t.lane, t.vec, t.lanes);
+  int8_t* qp = a.q + (m0 + r0 + t.lane) * a.ldq + t.vec * 8;
+  const int64_t step = t.lanes * a.ldq;
+  float* inverse = reinterpret_cast<float*>(scales + turn);
+  for (int i = threadIdx.x; i < turn; i += blockDim.x) scales[i] = 0;
+  __syncthreads();
+  int n = live && rows > t.lane ? (rows - t.lane + t.lanes - 1) / t.lanes : 0;  // rows left of this thread
+  uint4 v[kGnUnroll];
+#pragma unroll
+  for (int u = 0; u < kGnUnroll; ++u)
+    if (u < n) v[u] = src.next();
+  // lanes of this warp that share a row: those with the same t.lane; up to two such groups where a row has 32 vectors or more
+  const uint32_t peers = __match_any_sync(0xFFFFFFFFu, t.lane);
+  const uint32_t first = __shfl_sync(0xFFFFFFFFu, peers, 0);
+  const bool in_first = peers == first, two = t.vecs >= 32;
+  for (int base = 0; base < rows; base += turn, n -= kGnUnroll) {
+    uint64_t h[kGnUnroll][4];
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u) {
+      uint32_t mx = 0;
+      if (u < n) {
+        gn_unpack(v[u], h[u]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          h[u][j] = gn_act<SILU>(k.h(h[u][j], j));
+          mx = max(mx, max(static_cast<uint32_t>(h[u][j]) & 0x7FFFFFFFu, static_cast<uint32_t>(h[u][j] >> 32) & 0x7FFFFFFFu));
+        }
+        if (u + kGnUnroll < n) v[u] = src.next();
+      }
+      if (two) {
+        const uint32_t m1 = __reduce_max_sync(0xFFFFFFFFu, in_first ? mx : 0u), m2 = __reduce_max_sync(0xFFFFFFFFu, in_first ? 0u : mx);
+        if (live && (peers & ((1u << (threadIdx.x & 31)) - 1u)) == 0) atomicMax(scales + u * t.lanes + t.lane, in_first ? m1 : m2);
+      } else if (live) {
+        atomicMax(scales + u * t.lanes + t.lane, mx);
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < turn; i += blockDim.x) {
+      const float amax = __uint_as_float(scales[i]);
+      float sa = 0.0f, inv = 0.0f;
+      if (!(amax < 7.888609052210118e-31f)) {  // 2^-100, as in dp_daq_quantize
+        sa = __fdiv_rn(amax, 127.0f);
+        inv = __fdiv_rn(127.0f, amax);
+      }
+      inverse[i] = inv;
+      scales[i] = 0;
+      if (base + i < rows) a.s_a[m0 + r0 + base + i] = sa;
+    }
+    __syncthreads();  // (the next turn's maxima are behind it, its reciprocals behind the next but one)
+    const uint64_t magic2 = f32x2_pack(12582912.0f, 12582912.0f);
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u)
+      if (u < n) {
+        const float inv = inverse[u * t.lanes + t.lane];
+        const uint64_t inv2 = f32x2_pack(inv, inv);
+        uint32_t c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t w = f32x2_fma(h[u][j], inv2, magic2);
+          c[j] = __byte_perm(static_cast<uint32_t>(w), static_cast<uint32_t>(w >> 32), 0x0040);
+        }
+        *reinterpret_cast<uint2*>(qp) = make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410));
+        qp += step;
+      }
   }
 }
 
-// The same to codes: RW warps to a row (each lane up to three vectors), the row's absmax first.
-constexpr int kGnVecs = 3;
-template <int RW, bool SILU>
-__global__ void __launch_bounds__(kGnThreads) gn_codes_kernel(const GnArgs a) {
-  constexpr int TPR = 32 * RW, ROWS = kGnThreads / TPR;
-  extern __shared__ float gn_part[];  // [G][3]
-  __shared__ uint32_t gn_max[2][kGnThreads / 32];
+template <bool CODES, bool SILU, typename Source>
+__device__ __forceinline__ void gn_out(const GnArgs& a, const GnThread& t, const float* groups, uint32_t* scales, int64_t m0,
+                                       int64_t r0, int64_t r1, const Source& src) {
+  if constexpr (CODES) gn_codes<SILU>(a, t, groups, scales, m0, r0, r1, src);
+  else gn_write<SILU>(a, t, groups, m0, r0, r1, src);
+}
+// shared memory: the groups' (pivot, mean - pivot, rstd) and sums, gn_codes' scales; then gn_sums' part, then rows
+__host__ __device__ constexpr int gn_head_floats(int G, int lanes) { return (5 * G + 1 + 2 * kGnUnroll * lanes + 3) & ~3; }
+__device__ __forceinline__ uint32_t* gn_scales(const GnArgs& a) {
+  extern __shared__ __align__(16) float gn_smem[];
+  return reinterpret_cast<uint32_t*>(gn_smem + 5 * a.G + 1);
+}
+
+__global__ void __launch_bounds__(kGnMaxThreads) gn_stats_kernel(const GnArgs a) {
+  extern __shared__ __align__(16) float gn_smem[];
   pdl_launch_dependents();
+  const GnThread t(a.C);
   const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  const int64_t r0 = chunk * a.chunk_rows, r1 = min(r0 + a.chunk_rows, a.rows);
-  const int warp = threadIdx.x >> 5, rw = threadIdx.x / TPR, lane = threadIdx.x % TPR, vecs = a.C >> 3;
+  const int64_t r0 = chunk * a.chunk_rows;
   pdl_wait();
-  gn_groups(a, sample, gn_part);
+  gn_sums<false>(a, t, a.x + sample * a.rows * a.ldx, r0, min(r0 + a.chunk_rows, a.rows), gn_smem, nullptr,
+                 a.sums + static_cast<int64_t>(blockIdx.x) * a.G);
+}
+
+template <bool CODES, bool SILU>
+__global__ void __launch_bounds__(kGnMaxThreads) gn_apply_kernel(const GnArgs a) {
+  extern __shared__ __align__(16) float gn_smem[];
+  pdl_launch_dependents();
+  const GnThread t(a.C);
+  // the last chunks first: of maps beyond the L2 they are what is left there
+  const int block = gridDim.x - 1 - blockIdx.x, sample = block / a.chunks, chunk = block % a.chunks;
+  const int64_t r0 = chunk * a.chunk_rows, m0 = sample * a.rows;
+  const uint16_t* xs = a.x + m0 * a.ldx;
+  pdl_wait();
+  gn_groups(a, xs, a.chunks, gn_smem, [&](int c, int g) {
+    float2 v;
+    const float2* p = a.sums + (static_cast<int64_t>(sample) * a.chunks + c) * a.G + g;
+    asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
+    return v;
+  });
   __syncthreads();
-  float pv[kGnVecs][8], ca[kGnVecs][8], cb[kGnVecs][8];
-#pragma unroll
-  for (int i = 0; i < kGnVecs; ++i)
-    if (lane + TPR * i < vecs) gn_coefs(a, gn_part, (lane + TPR * i) * 8, pv[i], ca[i], cb[i]);
-  const int64_t m0 = sample * a.rows;
-  int it = 0;
-  for (int64_t base = r0; base < r1; base += ROWS, it ^= 1) {
-    const int64_t r = base + rw;
-    const bool live = r < r1;
-    float h[kGnVecs][8];
-    uint32_t mx = 0;
-    if (live) {
-      const uint16_t* xr = a.x + (m0 + r) * a.ldx;
-#pragma unroll
-      for (int i = 0; i < kGnVecs; ++i)
-        if (lane + TPR * i < vecs) {
-          gn_unpack(ld_global_v4(xr + (lane + TPR * i) * 8), h[i]);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            h[i][j] = gn_act<SILU>(fmaf(h[i][j] - pv[i][j], ca[i][j], cb[i][j]));
-            mx = max(mx, __float_as_uint(h[i][j]) & 0x7FFFFFFFu);
-          }
-        }
-    }
-    mx = __reduce_max_sync(0xFFFFFFFFu, mx);
-    if constexpr (RW > 1) {
-      if ((threadIdx.x & 31) == 0) gn_max[it][warp] = mx;
-      __syncthreads();  // (two buffers: the next row's maximum is written behind the next barrier's arrival only)
-#pragma unroll
-      for (int w = 0; w < RW; ++w) mx = max(mx, gn_max[it][rw * RW + w]);
-    }
-    if (!live) continue;
-    const float amax = __uint_as_float(mx);
-    float sa = 0.0f, inv = 0.0f;
-    if (!(amax < 7.888609052210118e-31f)) {  // 2^-100, as in dp_daq_quantize
-      sa = __fdiv_rn(amax, 127.0f);
-      inv = __fdiv_rn(127.0f, amax);
-    }
-    uint2* qr = reinterpret_cast<uint2*>(a.q + (m0 + r) * a.ldq);
-#pragma unroll
-    for (int i = 0; i < kGnVecs; ++i)
-      if (lane + TPR * i < vecs) {
-        uint32_t c[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = __float_as_uint(__fmaf_rn(h[i][j], inv, 12582912.0f));
-        qr[lane + TPR * i] = make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
-                                        __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
-      }
-    if (lane == 0) a.s_a[m0 + r] = sa;
-  }
+  gn_out<CODES, SILU>(a, t, gn_smem, gn_scales(a), m0, r0, min(r0 + a.chunk_rows, a.rows),
+                   GnFromGlobal{xs, a.ldx});
+}
+
+// One sample by a cluster of a.chunks CTAs, each with its rows in shared memory.
+template <bool CODES, bool SILU>
+__global__ void __launch_bounds__(kGnMaxThreads) gn_cluster_kernel(const GnArgs a) {
+  extern __shared__ __align__(16) float gn_smem[];
+  pdl_launch_dependents();
+  const GnThread t(a.C);
+  const int sample = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const int64_t r0 = min(chunk * a.chunk_rows, a.rows), r1 = min(r0 + a.chunk_rows, a.rows), m0 = sample * a.rows;
+  float* groups = gn_smem;
+  float2* sums = reinterpret_cast<float2*>(gn_smem + ((3 * a.G + 1) & ~1));
+  float* part = gn_smem + gn_head_floats(a.G, t.lanes);
+  uint4* rows_at = reinterpret_cast<uint4*>(part + 2 * t.lanes * a.C);
+  const uint16_t* xs = a.x + m0 * a.ldx;
+  pdl_wait();
+  gn_sums<true>(a, t, xs, r0, r1, part, rows_at, sums);
+  __syncwarp();
+  cluster_sync();
+  gn_groups(a, xs, a.chunks, groups, [&](int c, int g) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(map_to_cta(sums + g, c)) : "memory");
+    return v;
+  });
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (this CTA has read the others' sums)
+  gn_out<CODES, SILU>(a, t, groups, gn_scales(a), m0, r0, r1, GnFromShared{rows_at, r0, t.vecs});
+  __syncwarp();
+  cluster_wait();  // nobody leaves while its sums are read
 }
 
 // ---- host side -------------------------------------------------------------------------------------
+static int gn_threads(int32_t C) {  // whole rows of C / 8 vectors
+  const int vecs = C / 8;
+  return (kGnMaxThreads / vecs * vecs + 31) / 32 * 32;
+}
+static size_t gn_part_bytes(int32_t C) { return 2 * sizeof(float) * static_cast<size_t>(gn_threads(C) / (C / 8)) * C; }
+static int gn_head_bytes(int32_t C, int32_t G) { return static_cast<int>(sizeof(float)) * gn_head_floats(G, gn_threads(C) / (C / 8)); }
+
+// CTAs to a cluster of the one-kernel form, 0 where a sample does not fit.
+static int gn_cluster(int64_t samples, int64_t rows, int32_t C, int32_t G) {
+  const size_t room = kGnSmem - gn_head_bytes(C, G) - gn_part_bytes(C);
+  int cs = 1;
+  while (cs <= kGnMaxCluster && static_cast<size_t>((rows + cs - 1) / cs) * C * 2 > room) cs *= 2;
+  if (cs > kGnMaxCluster) return 0;
+  while (cs < kGnMaxCluster && samples * cs * 2 <= 148 && rows >= 4 * cs) cs *= 2;
+  return cs;
+}
 static int gn_chunks(int64_t samples, int64_t rows) {
-  // about four CTAs to an SM, 16 rows or more to each
-  int64_t c = (148 * 4 + samples - 1) / samples;
+  // about one CTA of 20 warps to an SM, 16 rows or more to each
+  int64_t c = 148 / samples;
   c = c < 1 ? 1 : c > kGnMaxChunks ? kGnMaxChunks : c;
   const int64_t most = (rows + 15) / 16;
   return static_cast<int>(c < most ? c : most < 1 ? 1 : most);
 }
-size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t G) {
-  if (samples <= 0 || rows <= 0) return 256;
+size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t C, int32_t G) {
+  if (samples <= 0 || rows <= 0 || C < 8 || gn_cluster(samples, rows, C, G) != 0) return 256;
   return (static_cast<size_t>(samples) * gn_chunks(samples, rows) * G * sizeof(float2) + 255) & ~static_cast<size_t>(255);
 }
 
-template <bool SILU>
-static cudaError_t launch_gn_codes(const GnArgs& a, dim3 grid, size_t smem, cudaStream_t stream) {
-  return a.C <= 768     ? launch(gn_codes_kernel<1, SILU>, grid, dim3(kGnThreads), smem, stream, true, a)
-         : a.C <= 768 * 2 ? launch(gn_codes_kernel<2, SILU>, grid, dim3(kGnThreads), smem, stream, true, a)
-         : a.C <= 768 * 4 ? launch(gn_codes_kernel<4, SILU>, grid, dim3(kGnThreads), smem, stream, true, a)
-                       : launch(gn_codes_kernel<8, SILU>, grid, dim3(kGnThreads), smem, stream, true, a);
+#define GN_PICK(KERNEL, codes, silu) \
+  ((codes) ? ((silu) ? KERNEL<true, true> : KERNEL<true, false>) : ((silu) ? KERNEL<false, true> : KERNEL<false, false>))
+
+int group_norm_init_device() {
+  for (bool codes : {false, true})
+    for (bool silu : {false, true})
+      DP_CUDA_OK(cudaFuncSetAttribute(GN_PICK(gn_cluster_kernel, codes, silu), cudaFuncAttributeMaxDynamicSharedMemorySize, kGnSmem));
+  return DP_OK;
 }
 
 int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, int64_t ldx, int32_t G, const void* gamma,
                       const void* beta, float eps, bool silu, void* y, int64_t ldy, int8_t* q, int64_t ldq, float* s_a,
                       void* workspace, cudaStream_t stream) {
-  GnArgs a{static_cast<const uint16_t*>(x), rows, ldx, C, G, static_cast<const uint16_t*>(gamma),
+  GnArgs a{static_cast<const uint16_t*>(x), rows, ldx, C, G, C / G, ((1ull << 32) + C / G - 1) / (C / G), static_cast<const uint16_t*>(gamma),
            static_cast<const uint16_t*>(beta), eps, static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
            static_cast<float2*>(workspace), 0, 0};
-  a.chunks = gn_chunks(samples, rows);
-  a.chunk_rows = (rows + a.chunks - 1) / a.chunks;
-  const int vecs = C / 8, threads = vecs > kGnThreads ? (vecs + 31) / 32 * 32 : kGnThreads;
-  const dim3 grid(static_cast<unsigned>(samples * a.chunks));
-  const size_t stats_smem = 2 * sizeof(float) * static_cast<size_t>(threads / vecs) * C, smem = 3 * sizeof(float) * static_cast<size_t>(G);
-  cudaError_t e = launch(gn_stats_kernel, grid, dim3(threads), stats_smem, stream, true, a);
-  if (e == cudaSuccess) {
-    if (q != nullptr) e = silu ? launch_gn_codes<true>(a, grid, smem, stream) : launch_gn_codes<false>(a, grid, smem, stream);
-    else e = silu ? launch(gn_apply_kernel<true>, grid, dim3(threads), smem, stream, true, a)
-                  : launch(gn_apply_kernel<false>, grid, dim3(threads), smem, stream, true, a);
+  const bool codes = q != nullptr;
+  const int threads = gn_threads(C);
+  const size_t head = gn_head_bytes(C, G), part = gn_part_bytes(C);
+  cudaError_t e = cudaSuccess;
+  if (const int cs = gn_cluster(samples, rows, C, G); cs != 0) {
+    a.chunks = cs;
+    a.chunk_rows = (rows + cs - 1) / cs;
+    e = launch_cluster(GN_PICK(gn_cluster_kernel, codes, silu), dim3(static_cast<unsigned>(samples * cs)), dim3(threads),
+                       head + part + static_cast<size_t>(a.chunk_rows) * C * 2, stream, true, static_cast<unsigned>(cs), a);
+  } else {
+    a.chunks = gn_chunks(samples, rows);
+    a.chunk_rows = (rows + a.chunks - 1) / a.chunks;
+    const dim3 grid(static_cast<unsigned>(samples * a.chunks));
+    e = launch(gn_stats_kernel, grid, dim3(threads), part, stream, true, a);
+    if (e == cudaSuccess) e = launch(GN_PICK(gn_apply_kernel, codes, silu), grid, dim3(threads), head, stream, true, a);
   }
   if (e != cudaSuccess) return fail(DP_ERR_CUDA, "group norm launch failed: %s", cudaGetErrorString(e));
   return DP_OK;
