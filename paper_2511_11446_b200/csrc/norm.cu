@@ -89,17 +89,21 @@ template <bool KEEP>
 __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, const uint16_t* xs, int64_t r0, int64_t r1, float* part,
                                         uint4* rows_at, float2* out) {
   if (t.lane < t.lanes) {
+    int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;  // rows of this thread
+    const uint16_t* xp = xs + (r0 + t.lane) * a.ldx + t.vec * 8;
+    uint4* keep = rows_at + t.lane * t.vecs + t.vec;
+    const int64_t step = t.lanes * a.ldx;
+    const int keep_step = t.lanes * t.vecs;
+    uint4 v[kGnUnroll];
+#pragma unroll
+    for (int u = 0; u < kGnUnroll; ++u, xp += step)
+      if (u < n) v[u] = ld_global_v4(xp);
     uint64_t s2[4], ss2[4], minus[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       s2[j] = ss2[j] = 0;
       minus[j] = f32x2_pack(-gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j) * a.per), -gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j + 1) * a.per));
     }
-    int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;  // rows of this thread
-    const uint16_t* xp = xs + (r0 + t.lane) * a.ldx + t.vec * 8;
-    uint4* keep = rows_at + t.lane * t.vecs + t.vec;
-    const int64_t step = t.lanes * a.ldx;
-    const int keep_step = t.lanes * t.vecs;
     auto add = [&](const uint4& v) {
       uint64_t f[4];
       gn_unpack(v, f);
@@ -111,10 +115,6 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
       }
     };
     // the next rows are on their way while these are added
-    uint4 v[kGnUnroll];
-#pragma unroll
-    for (int u = 0; u < kGnUnroll; ++u, xp += step)
-      if (u < n) v[u] = ld_global_v4(xp);
     for (; n > 0; n -= kGnUnroll) {
       uint4 nx[kGnUnroll];
 #pragma unroll
@@ -223,17 +223,10 @@ struct GnCoefs {
   uint64_t minus[4], a[4], b[4];
   __device__ __forceinline__ uint64_t h(uint64_t x, int j) const { return f32x2_fma(f32x2_add(x, minus[j]), a[j], b[j]); }
 };
-__device__ __forceinline__ void gn_coefs(const GnArgs& a, const float* groups, int c0, GnCoefs& k) {
+__device__ __forceinline__ void gn_coefs(const GnArgs& a, const float* groups, int c0, const uint4& gamma, const uint4& beta, GnCoefs& k) {
   uint64_t gm[4], bt[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    gm[j] = f32x2_pack(1.0f, 1.0f);
-    bt[j] = 0;
-  }
-  if (a.gamma != nullptr) {
-    gn_unpack(ld_global_v4(a.gamma + c0), gm);
-    gn_unpack(ld_global_v4(a.beta + c0), bt);
-  }
+  gn_unpack(gamma, gm);
+  gn_unpack(beta, bt);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float *g = groups + gn_group(a, c0 + 2 * j) * 3, *h = groups + gn_group(a, c0 + 2 * j + 1) * 3;
@@ -243,17 +236,40 @@ __device__ __forceinline__ void gn_coefs(const GnArgs& a, const float* groups, i
   }
 }
 
-// bf16 output of rows [r0, r1). Source: where a row's vectors are read, by next row of the thread.
-template <bool SILU, typename Source>
+// A thread's gamma and beta, on their way while the statistics are joined.
+struct GnAffine {
+  uint4 gamma, beta;
+  __device__ __forceinline__ GnAffine(const GnArgs& a, const GnThread& t) {
+    gamma = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);  // ones
+    beta = make_uint4(0, 0, 0, 0);
+    if (a.gamma != nullptr) {
+      gamma = ld_global_v4(a.gamma + t.vec * 8);
+      beta = ld_global_v4(a.beta + t.vec * 8);
+    }
+  }
+};
+__device__ __forceinline__ int gn_rows(const GnThread& t, int64_t r0, int64_t r1) {  // of this thread
+  const int rows = static_cast<int>(r1 - r0);
+  return t.lane < t.lanes && rows > t.lane ? (rows - t.lane + t.lanes - 1) / t.lanes : 0;
+}
+
+// bf16 output of rows [r0, r1). Source: where a row's vectors are read, by next row of the thread; the first ones fly before
+// ready(), which leaves the groups' statistics.
+template <bool SILU, typename Source, typename Ready>
 __device__ __forceinline__ void gn_write(const GnArgs& a, const GnThread& t, const float* groups, int64_t m0, int64_t r0, int64_t r1,
-                                         Source src) {
-  if (t.lane >= t.lanes) return;
-  GnCoefs k;
-  gn_coefs(a, groups, t.vec * 8, k);
-  int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;
+                                         Source src, Ready ready) {
+  int n = gn_rows(t, r0, r1);
   uint16_t* yp = a.y + (m0 + r0 + t.lane) * a.ldy + t.vec * 8;
   const int64_t step = t.lanes * a.ldy;
   src.start(r0 + t.lane, t.vec, t.lanes);
+  uint4 v[kGnUnroll];
+#pragma unroll
+  for (int u = 0; u < kGnUnroll; ++u)
+    if (u < n) v[u] = src.next();
+  const GnAffine affine(a, t);
+  ready();
+  GnCoefs k;
+  gn_coefs(a, groups, t.vec * 8, affine.gamma, affine.beta, k);
   auto put = [&](const uint4& v) {
     uint64_t f[4];
     gn_unpack(v, f);
@@ -267,10 +283,6 @@ __device__ __forceinline__ void gn_write(const GnArgs& a, const GnThread& t, con
     st_global_v4(yp, w);
     yp += step;
   };
-  uint4 v[kGnUnroll];
-#pragma unroll
-  for (int u = 0; u < kGnUnroll; ++u)
-    if (u < n) v[u] = src.next();
   for (; n > 0; n -= kGnUnroll) {
     uint4 nx[kGnUnroll];
 #pragma unroll
@@ -316,24 +328,26 @@ struct GnFromShared {
 // Codes of rows [r0, r1), kGnUnroll x lanes rows a turn: a thread's values of its rows stay in registers while the rows' maxima meet
 // in shared memory (warps first, then an atomic maximum each) and one thread a row makes scale and reciprocal of its. `scales`:
 // kGnUnroll x lanes pairs of (maximum, then reciprocal) words, zero before and after.
-template <bool SILU, typename Source>
+template <bool SILU, typename Source, typename Ready>
 __device__ __forceinline__ void gn_codes(const GnArgs& a, const GnThread& t, const float* groups, uint32_t* scales, int64_t m0,
-                                         int64_t r0, int64_t r1, Source src) {
+                                         int64_t r0, int64_t r1, Source src, Ready ready) {
   const bool live = t.lane < t.lanes;
   const int rows = static_cast<int>(r1 - r0), turn = kGnUnroll * t.lanes;
-  GnCoefs k;
-  gn_coefs(a, groups, t.vec * 8, k);
   src.start(r0 + t.lane, t.vec, t.lanes);
   int8_t* qp = a.q + (m0 + r0 + t.lane) * a.ldq + t.vec * 8;
   const int64_t step = t.lanes * a.ldq;
   float* inverse = reinterpret_cast<float*>(scales + turn);
   for (int i = threadIdx.x; i < turn; i += blockDim.x) scales[i] = 0;
-  __syncthreads();
-  int n = live && rows > t.lane ? (rows - t.lane + t.lanes - 1) / t.lanes : 0;  // rows left of this thread
+  int n = gn_rows(t, r0, r1);  // left of this thread's
   uint4 v[kGnUnroll];
 #pragma unroll
   for (int u = 0; u < kGnUnroll; ++u)
     if (u < n) v[u] = src.next();
+  const GnAffine affine(a, t);
+  ready();
+  __syncthreads();
+  GnCoefs k;
+  gn_coefs(a, groups, t.vec * 8, affine.gamma, affine.beta, k);
   // lanes of this warp that share a row: those with the same t.lane; up to two such groups where a row has 32 vectors or more
   const uint32_t peers = __match_any_sync(0xFFFFFFFFu, t.lane);
   const uint32_t first = __shfl_sync(0xFFFFFFFFu, peers, 0);
@@ -390,11 +404,11 @@ __device__ __forceinline__ void gn_codes(const GnArgs& a, const GnThread& t, con
   }
 }
 
-template <bool CODES, bool SILU, typename Source>
+template <bool CODES, bool SILU, typename Source, typename Ready>
 __device__ __forceinline__ void gn_out(const GnArgs& a, const GnThread& t, const float* groups, uint32_t* scales, int64_t m0,
-                                       int64_t r0, int64_t r1, const Source& src) {
-  if constexpr (CODES) gn_codes<SILU>(a, t, groups, scales, m0, r0, r1, src);
-  else gn_write<SILU>(a, t, groups, m0, r0, r1, src);
+                                       int64_t r0, int64_t r1, const Source& src, Ready ready) {
+  if constexpr (CODES) gn_codes<SILU>(a, t, groups, scales, m0, r0, r1, src, ready);
+  else gn_write<SILU>(a, t, groups, m0, r0, r1, src, ready);
 }
 // shared memory: the groups' (pivot, mean - pivot, rstd) and sums, gn_codes' scales; then gn_sums' part, then rows
 __host__ __device__ constexpr int gn_head_floats(int G, int lanes) { return (5 * G + 1 + 2 * kGnUnroll * lanes + 3) & ~3; }
@@ -424,15 +438,15 @@ __global__ void __launch_bounds__(kGnMaxThreads) gn_apply_kernel(const GnArgs a)
   const int64_t r0 = chunk * a.chunk_rows, m0 = sample * a.rows;
   const uint16_t* xs = a.x + m0 * a.ldx;
   pdl_wait();
-  gn_groups(a, xs, a.chunks, gn_smem, [&](int c, int g) {
-    float2 v;
-    const float2* p = a.sums + (static_cast<int64_t>(sample) * a.chunks + c) * a.G + g;
-    asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
-    return v;
+  gn_out<CODES, SILU>(a, t, gn_smem, gn_scales(a), m0, r0, min(r0 + a.chunk_rows, a.rows), GnFromGlobal{xs, a.ldx}, [&]() {
+    gn_groups(a, xs, a.chunks, gn_smem, [&](int c, int g) {
+      float2 v;
+      const float2* p = a.sums + (static_cast<int64_t>(sample) * a.chunks + c) * a.G + g;
+      asm volatile("ld.global.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
+      return v;
+    });
+    __syncthreads();
   });
-  __syncthreads();
-  gn_out<CODES, SILU>(a, t, gn_smem, gn_scales(a), m0, r0, min(r0 + a.chunk_rows, a.rows),
-                   GnFromGlobal{xs, a.ldx});
 }
 
 // One sample by a cluster of a.chunks CTAs, each with its rows in shared memory.
@@ -450,16 +464,17 @@ __global__ void __launch_bounds__(kGnMaxThreads) gn_cluster_kernel(const GnArgs 
   const uint16_t* xs = a.x + m0 * a.ldx;
   pdl_wait();
   gn_sums<true>(a, t, xs, r0, r1, part, rows_at, sums);
-  __syncwarp();
-  cluster_sync();
-  gn_groups(a, xs, a.chunks, groups, [&](int c, int g) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(map_to_cta(sums + g, c)) : "memory");
-    return v;
+  gn_out<CODES, SILU>(a, t, groups, gn_scales(a), m0, r0, r1, GnFromShared{rows_at, r0, t.vecs}, [&]() {
+    __syncwarp();
+    cluster_sync();
+    gn_groups(a, xs, a.chunks, groups, [&](int c, int g) {
+      float2 v;
+      asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(map_to_cta(sums + g, c)) : "memory");
+      return v;
+    });
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (this CTA has read the others' sums)
   });
-  __syncthreads();
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (this CTA has read the others' sums)
-  gn_out<CODES, SILU>(a, t, groups, gn_scales(a), m0, r0, r1, GnFromShared{rows_at, r0, t.vecs});
   __syncwarp();
   cluster_wait();  // nobody leaves while its sums are read
 }
