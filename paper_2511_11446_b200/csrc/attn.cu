@@ -17,7 +17,9 @@ namespace dp {
 
 constexpr int kAtThreads = 128, kAtKeys = 64;
 constexpr int kAtMaxSplits = 8;  // CTAs of a cluster
-constexpr int kFewKeys = 32, kFewStages = 2;  // of a warp's ring
+constexpr int kFewKeys = 32;  // of a stage of a warp's ring
+// Stages of that ring: two CTAs to an SM (45 to 90 KB each).
+__host__ __device__ constexpr int few_stages(int dp) { return dp <= 96 ? 2 : 1; }
 
 // Bytes between the rows of a tile in shared memory: an odd number of 16-byte units, so that the eight rows of a matrix that
 // ldmatrix fetches lie in different banks.
@@ -52,26 +54,45 @@ __device__ __forceinline__ void ld_cluster_f32x2(uint32_t a, float& x, float& y)
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(a) : "memory");
 }
 
-// What both kernels do with a fragment of 16 rows x N keys of scores: scaled, capped, biased, masked, in log2 units; the rows' new
-// maxima (of the four lanes that share a row) into mx.
 struct AtRows {
   int tok[2], pos[2];  // of fragment rows lane / 4 and lane / 4 + 8 (tok < 0: none)
+  int bound[2];        // keys below it are visible
   float slope[2];
 };
+// What both kernels do with a fragment of 16 rows x 8 N keys of scores: scaled, capped, biased, masked, in log2 units; the rows'
+// new maxima (of the four lanes that share a row) into mx. tile_end: behind the fragment's last key.
 template <int N>
-__device__ __forceinline__ void at_scores(const AttnParams& p, const AttnSeq& s, const AtRows& w, int keys, int key0, float (&sc)[N][4],
+__device__ __forceinline__ void at_scores(const AttnParams& p, const AtRows& w, int key0, int tile_end, float (&sc)[N][4],
                                           float (&mx)[2]) {
+  if (p.cap != 0.0f) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[n][i] = capped(p.cap, sc[n][i] * p.scale_by_cap);
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[n][i] *= p.scale;
+  }
+  if (p.slopes != nullptr) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        sc[n][i] = fmaf(-w.slope[i >> 1], fabsf(static_cast<float>(w.pos[i >> 1] - (key0 + n * 8 + (i & 1)))), sc[n][i]);
+  }
+  if (__any_sync(0xFFFFFFFFu, tile_end > min(w.bound[0], w.bound[1]))) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (key0 + n * 8 + (i & 1) >= w.bound[i >> 1]) sc[n][i] = -INFINITY;
+  }
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = i >> 1, key = key0 + n * 8 + (i & 1);
-      float x = p.cap != 0.0f ? capped(p.cap, sc[n][i] * p.scale_by_cap) : sc[n][i] * p.scale;
-      if (p.slopes != nullptr) x = fmaf(-w.slope[e], fabsf(static_cast<float>(w.pos[e] - key)), x);
-      if (key >= keys || (p.causal && key > w.pos[e] && key >= s.prefix)) x = -INFINITY;
-      sc[n][i] = x;
-      mx[e] = fmaxf(mx[e], x);
-    }
+    for (int i = 0; i < 4; ++i) mx[i >> 1] = fmaxf(mx[i >> 1], sc[n][i]);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xFFFFFFFFu, mx[e], 1));
@@ -90,6 +111,8 @@ __device__ __forceinline__ void at_rows(const AttnParams& p, const AttnSeq& s, i
     w.tok[e] = live ? static_cast<int>(row / group) : -1;
     const int head = kvh * group + (live ? static_cast<int>(row % group) : 0);
     w.pos[e] = w.tok[e] + s.behind;
+    w.bound[e] = p.causal ? min(s.nk, max(w.pos[e] + 1, s.prefix)) : s.nk;
+    if (!live) w.bound[e] = 0x7FFFFFFF;  // (nobody's row: nothing to be masked)
     w.slope[e] = p.slopes != nullptr ? ld_global_f32(p.slopes + head) * kLog2e : 0.0f;
     const uint16_t* qr = p.q + static_cast<int64_t>(s.q0 + (live ? w.tok[e] : 0)) * p.ldq + head * p.q_hs;
 #pragma unroll
@@ -110,7 +133,7 @@ template <int DP, int MB>
 __global__ void __launch_bounds__(kAtThreads)
 attn_few_kernel(const AttnParams p, const int splits) {
   constexpr int ROWS = 16 * MB, RB = at_row_bytes(DP), KS = DP / 16, NB = DP / 8, OW = DP + 4;
-  constexpr int STAGE = 2 * kFewKeys * RB;
+  constexpr int STAGE = 2 * kFewKeys * RB, kFewStages = few_stages(DP);
   extern __shared__ __align__(128) uint8_t at_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
@@ -131,23 +154,33 @@ attn_few_kernel(const AttnParams p, const int splits) {
   const int begin = static_cast<int>(static_cast<int64_t>(n) * part_at / parts), end = static_cast<int>(static_cast<int64_t>(n) * (part_at + 1) / parts);
   const uint16_t* kp = p.k + static_cast<int64_t>(s.k0) * p.ldk + kvh * p.k_hs;
   const uint16_t* vp = p.v + static_cast<int64_t>(s.k0) * p.ldv + kvh * p.v_hs;
-  const int vecs = p.D / 8, dr = 32 / vecs, dc = 32 % vecs;  // a step of 32 vectors in rows and vectors
+  const int vecs = p.D / 8;
   const uint32_t ring0 = smem_u32(ring);
+  // The tile's 16-byte pieces in the order of memory, one a lane: a warp's request then covers few lines. (Two lanes to a key and
+  // 32 bytes at a time needs less arithmetic and is slower, 49 us against 37: every request touches 16 lines.) A piece's successor
+  // is 32 pieces on: dr rows and dc pieces, one row more where those pass the row's end.
+  const int r_first = lane / vecs, c_first = lane % vecs, dr = 32 / vecs, dc = 32 % vecs;
+  const int64_t k_on = dr * p.ldk + dc * 8, k_wrap = k_on + p.ldk - vecs * 8, v_on = dr * p.ldv + dc * 8, v_wrap = v_on + p.ldv - vecs * 8;
+  const int dst_on = dr * RB + dc * 16, dst_wrap = dst_on + RB - vecs * 16;
   auto load = [&](int t) {
-    const uint32_t dst = ring0 + ((t - begin) % kFewStages) * STAGE;
-    int r = lane / vecs, c = lane % vecs;
-    for (; r < kFewKeys;) {
-      const int64_t key = static_cast<int64_t>(t) * kFewKeys + r;
-      const bool ok = key < keys;  // rows behind the sequence belong to others: zeros in their place
-      const int64_t kk = ok ? key : 0;
-      cp_async_16(dst + r * RB + c * 16, kp + kk * p.ldk + c * 8, ok);
-      cp_async_16(dst + (kFewKeys + r) * RB + c * 16, vp + kk * p.ldv + c * 8, ok);
-      r += dr;
+    uint32_t dst = ring0 + ((t - begin) % kFewStages) * STAGE + r_first * RB + c_first * 16;
+    const int64_t row = static_cast<int64_t>(t) * kFewKeys + r_first;
+    const uint16_t *ks = kp + row * p.ldk + c_first * 8, *vs = vp + row * p.ldv + c_first * 8;
+    int c = c_first, r = r_first;
+    const int left = keys - t * kFewKeys;  // keys of this tile
+    // rows behind the sequence belong to others: zeros in their place (and the first key's address, which exists)
+#pragma unroll 2
+    for (int i = 0; i < vecs * kFewKeys / 32; ++i) {
+      const bool ok = r < left;
+      cp_async_16(dst, ok ? ks : kp, ok);
+      cp_async_16(dst + kFewKeys * RB, ok ? vs : vp, ok);
       c += dc;
-      if (c >= vecs) {
-        c -= vecs;
-        ++r;
-      }
+      const bool wrap = c >= vecs;
+      c -= wrap ? vecs : 0;
+      r += dr + wrap;
+      dst += wrap ? dst_wrap : dst_on;
+      ks += wrap ? k_wrap : k_on;
+      vs += wrap ? v_wrap : v_on;
     }
   };
 #pragma unroll
@@ -187,7 +220,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
           mma_16816(sc[2 * n2 + 1], qf[b][k], f[2], f[3]);
         }
       float mx[2] = {m[b][0], m[b][1]}, sub[2];
-      at_scores(p, s, w[b], keys, t * kFewKeys + (lane & 3) * 2, sc, mx);
+      at_scores(p, w[b], t * kFewKeys + (lane & 3) * 2, (t + 1) * kFewKeys, sc, mx);
       if (__any_sync(0xFFFFFFFFu, mx[0] != m[b][0] || mx[1] != m[b][1])) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -374,7 +407,7 @@ attn_rows_kernel(const AttnParams p, const int tiles) {
         mma_16816(sc[2 * n2 + 1], qf[k], f[2], f[3]);
       }
     float mx[2] = {m[0], m[1]}, sub[2];
-    at_scores(p, s, w, keys, t * kAtKeys + (lane & 3) * 2, sc, mx);
+    at_scores(p, w, t * kAtKeys + (lane & 3) * 2, (t + 1) * kAtKeys, sc, mx);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       sub[e] = mx[e] == -INFINITY ? 0.0f : mx[e];  // (no key in sight so far)
@@ -431,7 +464,7 @@ template <int DP>
 constexpr size_t at_rows_smem() { return static_cast<size_t>(kAtStages) * at_stage_bytes(DP); }
 template <int DP, int MB>
 constexpr size_t at_few_smem() {
-  constexpr size_t ring = 4 * static_cast<size_t>(kFewStages) * 2 * kFewKeys * at_row_bytes(DP);
+  constexpr size_t ring = 4 * static_cast<size_t>(few_stages(DP)) * 2 * kFewKeys * at_row_bytes(DP);
   constexpr size_t join = 5 * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
   return ring > join ? ring : join;
 }
@@ -466,8 +499,8 @@ int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t tiles = few ? 0 : (rows + 63) / 64;
   const int64_t units = (few ? 1 : tiles) * p.KV * p.n_seq;
   int splits = 1;
-  if (few) {  // as many CTAs as the SMs hold (two, of 64 to 136 KB each), as long as a warp has a tile of keys
-    const int64_t key_tiles = (static_cast<int64_t>(p.max_k) + kFewKeys - 1) / kFewKeys, most = (p.D <= 96 ? 2 : 1) * num_sms() / units;
+  if (few) {  // as many CTAs as the SMs hold, two each, as long as a warp has a tile of keys
+    const int64_t key_tiles = (static_cast<int64_t>(p.max_k) + kFewKeys - 1) / kFewKeys, most = 2 * num_sms() / units;
     splits = static_cast<int>(key_tiles / 4 < most ? key_tiles / 4 : most);
     splits = splits < 1 ? 1 : splits > kAtMaxSplits ? kAtMaxSplits : splits;
   }
