@@ -495,7 +495,9 @@ static cudaError_t launch_at(const AttnParams& p, unsigned grid, int tiles, int 
 
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
-  const bool few = rows <= 32;
+  // With a tile of keys or less there is nothing to split: the kernel whose warps share it (256 sequences of 32, 16 heads of 72:
+  // 48 us against 87).
+  const bool few = rows <= 32 && p.max_k > kAtKeys;
   const int64_t tiles = few ? 0 : (rows + 63) / 64;
   const int64_t units = (few ? 1 : tiles) * p.KV * p.n_seq;
   int splits = 1;

@@ -37,6 +37,8 @@ constexpr int kTcRegsLaunch = 168, kTcRegsSoftmax = 208, kTcRegsRest = 88;
 static_assert(256 * kTcRegsSoftmax + 128 * kTcRegsRest == kTcThreads * kTcRegsLaunch, "register split");
 constexpr float kTcRise = 8.0f;                   // log2 units by which a row's maximum may outgrow the reference
 
+constexpr int kTcOrderBytes = 784;                // of a TcOrder, a multiple of 16
+
 // Tiles for vectors of up to 16 KS elements.
 template <int KS>
 struct TcForm {
@@ -48,8 +50,8 @@ struct TcForm {
   static constexpr uint32_t kS = 0, kP = kBeside ? 2 * BN : 0, kPStep = kBeside ? BN / 2 : BN;
   static constexpr uint32_t kO = kBeside ? 3 * BN : 2 * BN;      // columns
   static_assert(kO + 2 * D <= 512, "tensor memory");
-  // (after the tiles: the ring of items, barriers, turns, tensor memory's address, the abort flag)
-  static constexpr size_t kSmem = 1024 + 2 * kQBytes + NS * kKvBytes + 4 * 48 + (2 * NS + 12 + 2 * 4) * 8 + 48;
+  // (after the tiles: the ring of items, the sequences' order, barriers, turns, tensor memory's address, the abort flag)
+  static constexpr size_t kSmem = 1024 + 2 * kQBytes + NS * kKvBytes + 4 * 48 + kTcOrderBytes + (2 * NS + 12 + 2 * 4) * 8 + 48;
   static_assert(kSmem <= 232448, "shared memory");
 };
 
@@ -58,6 +60,7 @@ struct AttnTcSched {
   int32_t tiles;       // items of the longest sequence
   int32_t items;       // tiles * heads * sequences
   int32_t group;       // (sequence, head) pairs whose items are taken together, longest ones first
+  int32_t sorted;      // sequences by their keys instead, and no items that are not there (up to kTcSorted packed sequences)
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint64_t* bar) {
@@ -227,17 +230,12 @@ struct __align__(16) TcItem {
   int live0, live1;  // queries in them
   __device__ __forceinline__ int n() const { return max(n0, n1); }
 };
+constexpr int kTcSorted = 64;
 constexpr int kTcSlots = 4;      // of the ring of items
 constexpr int kTcItemReaders = 11;  // loads, two issuing threads, eight warps
 template <int BN>
-__device__ __forceinline__ bool tc_item(const AttnParams& p, const AttnTcSched& c, int item, TcItem& r) {
-  // pairs in groups; within a group the last rows, which see the most keys under a causal mask, come first
-  const int pairs = p.H * p.n_seq;
-  const int g = item / (c.group * c.tiles), in = item - g * c.group * c.tiles;
-  const int size = min(c.group, pairs - g * c.group);
-  const int tile = c.tiles - 1 - in / size, pair = g * c.group + in % size;
-  const int seq = pair / p.H;
-  r.head = pair - seq * p.H;
+__device__ __forceinline__ bool tc_item(const AttnParams& p, const AttnTcSched& c, int seq, int head, int tile, TcItem& r) {
+  r.head = head;
   r.s = attn_seq(p, seq);
   r.row0 = tile * c.rows;
   if (r.row0 >= r.s.nq) return false;
@@ -247,16 +245,75 @@ __device__ __forceinline__ bool tc_item(const AttnParams& p, const AttnTcSched& 
   r.n1 = r.live1 > 0 ? (attn_keys(p, r.s, r.row0 + kTcTile + r.live1 - 1) + BN - 1) / BN : 0;
   return true;
 }
+// Sequences in the order of their keys, most first, for packed ones of unlike lengths: order[rank] the sequence and its items per head,
+// start[rank] the items before it. By one warp.
+struct TcOrder {
+  int seq[kTcSorted], tiles[kTcSorted], start[kTcSorted + 1];
+};
+static_assert(sizeof(TcOrder) <= kTcOrderBytes, "sequences' order");
+__device__ __forceinline__ void tc_sort(const AttnParams& p, const AttnTcSched& c, TcOrder& o) {
+  const int lane = threadIdx.x & 31;
+  int keys[2], tiles[2], rank[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    keys[i] = -1;
+    tiles[i] = 0;
+    if (lane + 32 * i < p.n_seq) {
+      const AttnSeq s = attn_seq(p, lane + 32 * i);
+      keys[i] = s.nk;
+      tiles[i] = (s.nq + c.rows - 1) / c.rows;
+    }
+  }
+  for (int k = 0; k < kTcSorted; ++k) {
+    const int other = __shfl_sync(0xFFFFFFFFu, k < 32 ? keys[0] : keys[1], k & 31);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rank[i] += other > keys[i] || (other == keys[i] && k < lane + 32 * i);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    o.seq[rank[i]] = lane + 32 * i;
+    o.tiles[rank[i]] = tiles[i];
+  }
+  __syncwarp();
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int mine = o.tiles[lane + 32 * i] * p.H;
+    int sum = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+      if (lane >= d) sum += x;
+    }
+    o.start[lane + 32 * i] = before + sum - mine;
+    before += __shfl_sync(0xFFFFFFFFu, sum, 31);
+  }
+  if (lane == 0) o.start[kTcSorted] = before;
+  __syncwarp();
+}
 // The next item of this CTA: rounds of gridDim.x items, every other one backwards, so that the long items that come first
-// even out. False: there is none.
+// even out. `rank`: where the last one was found. False: there is none.
 template <int BN>
-__device__ __forceinline__ bool tc_next(const AttnParams& p, const AttnTcSched& c, int& round, TcItem& it) {
+__device__ __forceinline__ bool tc_next(const AttnParams& p, const AttnTcSched& c, const TcOrder& o, int& round, int& rank, TcItem& it) {
+  const int items = c.sorted ? o.start[kTcSorted] : c.items;
   for (;;) {
     const int64_t base = static_cast<int64_t>(round) * gridDim.x;
-    if (base >= c.items) return false;
-    const int64_t i = base + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (base >= items) return false;
+    const int64_t at = base + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
     ++round;
-    if (i < c.items && tc_item<BN>(p, c, static_cast<int>(i), it)) return true;
+    if (at >= items) continue;
+    const int i = static_cast<int>(at);
+    if (c.sorted) {  // (items of later rounds stand behind those of earlier ones)
+      while (o.start[rank + 1] <= i) ++rank;
+      const int in = i - o.start[rank], tile = in / p.H;
+      if (tc_item<BN>(p, c, o.seq[rank], in - tile * p.H, tile, it)) return true;
+    } else {
+      // pairs in groups; within a group the last rows, which see the most keys under a causal mask, come first
+      const int pairs = p.H * p.n_seq, g = i / (c.group * c.tiles), in = i - g * c.group * c.tiles;
+      const int size = min(c.group, pairs - g * c.group), from_last = in / size;
+      const int pair = g * c.group + in - from_last * size, seq = pair / p.H;
+      if (tc_item<BN>(p, c, seq, pair - seq * p.H, c.tiles - 1 - from_last, it)) return true;
+    }
   }
 }
 
@@ -271,7 +328,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
   uint8_t* sQ = smem;                    // [2][NBLK][128 rows][128 bytes]
   uint8_t* sKV = sQ + 2 * F::kQBytes;    // [NS][NBLK][BN rows][128 bytes]
   TcItem* slots = reinterpret_cast<TcItem*>(sKV + NS * F::kKvBytes);
-  uint64_t* full = reinterpret_cast<uint64_t*>(slots + kTcSlots);
+  TcOrder* order = reinterpret_cast<TcOrder*>(slots + kTcSlots);
+  uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(order) + kTcOrderBytes);
   uint64_t* empty = full + NS;
   uint64_t* item_full = empty + NS;
   uint64_t* item_empty = item_full + kTcSlots;
@@ -370,18 +428,21 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         }
       }
       if (!ok) producer_drain();
-    } else if (warp == 11 && elect_one()) {
+    } else if (warp == 11) {
       // ================= work items =================
-      int round = 0;
+      int round = 0, rank = 0;
+      if (c.sorted) tc_sort(p, c, *order);
       TcItem it;
-      bool ok = true, more = true;
-      while (ok && more) {
-        more = tc_next<BN>(p, c, round, it);
-        if (!more) it.row0 = -1;
-        if (!(ok = mbar_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag))) break;
-        slots[item_at.s] = it;
-        mbar_arrive(&item_full[item_at.s]);
-        item_at.next(kTcSlots);
+      if (elect_one()) {
+        bool ok = true, more = true;
+        while (ok && more) {
+          more = tc_next<BN>(p, c, *order, round, rank, it);
+          if (!more) it.row0 = -1;
+          if (!(ok = mbar_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag))) break;
+          slots[item_at.s] = it;
+          mbar_arrive(&item_full[item_at.s]);
+          item_at.next(kTcSlots);
+        }
       }
     } else if ((warp == 9 || warp == 10) && elect_one()) {
       // ================= products of tile t =================
@@ -665,6 +726,8 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   c.tiles = static_cast<int32_t>(tiles);
   c.items = static_cast<int32_t>(tiles * pairs);
   // Without a mask all items are alike and a pair's stand together, for its K and V in L2; with one, 64 pairs.
+  // Packed sequences are taken longest first, and only items that are there: 16 documents of 1 to 1500 tokens.
+  c.sorted = !p.causal && p.q_start != nullptr && p.n_seq <= kTcSorted;
   const int64_t group = p.causal ? 64 : 1;
   c.group = static_cast<int32_t>(group < pairs ? group : pairs);
   const unsigned ctas = static_cast<unsigned>(c.items < sms ? c.items : sms);
