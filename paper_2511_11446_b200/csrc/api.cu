@@ -609,8 +609,8 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   if (a->mask != DP_MASK_NONE && a->mask != DP_MASK_CAUSAL) return fail(DP_ERR_INVALID_ARG, "dp_attention: mask=%d", a->mask);
   if (a->prefix != nullptr && a->mask != DP_MASK_CAUSAL)
     return fail(DP_ERR_INVALID_ARG, "dp_attention: a prefix goes with DP_MASK_CAUSAL");
-  if (!(a->scale >= 0.0f) || !(a->scale <= 3.0e38f) || !(a->cap >= 0.0f) || !(a->cap <= 1.0e30f))
-    return fail(DP_ERR_INVALID_ARG, "dp_attention: scale=%g cap=%g must be finite and not negative", a->scale, a->cap);
+  if (!(a->scale >= 0.0f) || !(a->scale <= 3.0e38f) || !(a->cap >= 0.0f) || !(a->cap <= 65536.0f))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: scale=%g must be finite and not negative, cap=%g in [0, 65536]", a->scale, a->cap);
   const int64_t qh = a->q_head_stride ? a->q_head_stride : D, kh = a->k_head_stride ? a->k_head_stride : D;
   const int64_t vh = a->v_head_stride ? a->v_head_stride : D, yh = a->y_head_stride ? a->y_head_stride : D;
   constexpr int64_t kMaxStride = 1ll << 38;  // elements: a tensor map's strides stay below 2^40 bytes
@@ -646,7 +646,7 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   const double log2e = 1.4426950408889634074;
   p.scale = fmaxf(static_cast<float>(a->scale * log2e), 1.2e-38f);  // (of a hidden score, -inf, also where scale is 0)
   p.cap = static_cast<float>(a->cap * log2e);
-  p.scale_by_cap = a->cap != 0.0f ? static_cast<float>(2.0 * log2e * a->scale / a->cap) : 0.0f;
+  p.scale_by_cap = a->cap != 0.0f ? static_cast<float>(fmin(2.0 * log2e * a->scale / a->cap, 3.0e38)) : 0.0f;
   p.causal = a->mask == DP_MASK_CAUSAL;
   p.status = device_status;
   // A tile of 128 queries on tcgen05 beats 16-row fragments as soon as there is more than a handful of either: 8 x 40 queries over

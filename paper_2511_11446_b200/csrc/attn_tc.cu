@@ -57,9 +57,27 @@ struct AttnTcSched {
   int32_t tiles;       // items of the longest sequence
   int32_t items;       // tiles * heads * sequences
   int32_t group;       // (sequence, head) pairs whose items are taken together, longest ones first
+  int64_t budget;      // cycles that a wait may take
   int32_t sorted;      // sequences by their keys instead, and no items that are not there (up to kTcSorted packed sequences)
 };
 
+// mbar_wait with a limit that goes by the call: a warp of one tile of queries may wait for the other tile's whole item, and the
+// item ring for a few of them, so the limit grows with the keys.
+__device__ __forceinline__ bool tc_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int64_t budget) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  uint32_t polls = 0;
+  while (!mbar_try_wait(bar, parity)) {
+    if ((++polls & 63u) == 0) {
+      if (*abort_flag) return false;
+      if (clock64() - t0 > budget) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+  return true;
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -384,7 +402,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
   // The next item from the ring; `leader`: the thread that gives the slot back once all that read it with this one have.
   Ring item_at;
   auto next_item = [&](TcItem& it, bool warp_wide) {
-    bool ok = mbar_wait(&item_full[item_at.s], item_at.ph, abort_flag);
+    bool ok = tc_wait(&item_full[item_at.s], item_at.ph, abort_flag, c.budget);
     if (warp_wide) ok = __all_sync(0xFFFFFFFFu, ok);
     if (!ok) {
       it.row0 = -1;
@@ -407,7 +425,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       TcItem it;
       const uint32_t group = p.H / p.KV;
       auto load_q = [&](int t) {
-        if (!(ok = mbar_wait(&q_empty[t], (items[t] & 1) ^ 1u, abort_flag))) return;
+        if (!(ok = tc_wait(&q_empty[t], (items[t] & 1) ^ 1u, abort_flag, c.budget))) return;
         ++items[t];
         mbar_arrive_expect_tx(&q_full[t], F::kQBytes);
 #pragma unroll
@@ -419,7 +437,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         if (it.n0 > 0) load_q(0);
         const int kvh = it.head / group;
         for (int j = 0; j < 2 * n && ok; ++j) {  // K, V, K, V, ..
-          if (!(ok = mbar_wait(&empty[st.s], st.ph ^ 1u, abort_flag))) break;
+          if (!(ok = tc_wait(&empty[st.s], st.ph ^ 1u, abort_flag, c.budget))) break;
           mbar_arrive_expect_tx(&full[st.s], F::kKvBytes);
 #pragma unroll
           for (int b = 0; b < NBLK; ++b)
@@ -440,7 +458,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         while (ok && more) {
           more = tc_next<BN>(p, c, *order, round, rank, it);
           if (!more) it.row0 = -1;
-          if (!(ok = mbar_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag))) break;
+          if (!(ok = tc_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag, c.budget))) break;
           slots[item_at.s] = it;
           mbar_arrive(&item_full[item_at.s]);
           item_at.next(kTcSlots);
@@ -457,8 +475,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       uint32_t n_s = 0, n_p = 0, items = 0;  // scores, weights, items so far
       // Scores of the key tile in stage k into S, which the warpgroup has read.
       auto scores = [&](const Ring& k) {
-        if (n_s > 0 && !(ok = mbar_wait(&s_read[t], (n_s - 1) & 1, abort_flag))) return;
-        if (!(ok = mbar_wait(&full[k.s], k.ph, abort_flag))) return;
+        if (n_s > 0 && !(ok = tc_wait(&s_read[t], (n_s - 1) & 1, abort_flag, c.budget))) return;
+        if (!(ok = tc_wait(&full[k.s], k.ph, abort_flag, c.budget))) return;
         tc_fence_after();
         const uint64_t kd = k_desc + static_cast<uint64_t>(k.s * (F::kKvBytes >> 4));
 #pragma unroll
@@ -470,7 +488,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         ++n_s;
       };
       auto first_scores = [&](const Ring& k, int n) {  // of an item with n key tiles for this tile
-        if (!(ok = mbar_wait(&q_full[t], items & 1, abort_flag))) return;
+        if (!(ok = tc_wait(&q_full[t], items & 1, abort_flag, c.budget))) return;
         ++items;
         scores(k);
         if (ok && n == 1) mma_commit(&q_empty[t]);
@@ -494,7 +512,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
               if (ok && j + 2 == n) mma_commit(&q_empty[t]);
             };
             if (j + 1 < n) next_scores();
-            if (!ok || !(ok = mbar_wait(&p_full[t], n_p & 1, abort_flag)) || !(ok = mbar_wait(&full[v.s], v.ph, abort_flag))) break;
+            if (!ok || !(ok = tc_wait(&p_full[t], n_p & 1, abort_flag, c.budget)) || !(ok = tc_wait(&full[v.s], v.ph, abort_flag, c.budget))) break;
             ++n_p;
             tc_fence_after();
             const uint64_t vd = v_desc + static_cast<uint64_t>(v.s * (F::kKvBytes >> 4));
@@ -514,7 +532,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         }
         // the rest of the item's tiles is the other tile's: passed on as they come
         for (int j = 2 * n; j < 2 * n_all && ok; ++j) {
-          if (!(ok = mbar_wait(&full[st.s], st.ph, abort_flag))) break;
+          if (!(ok = tc_wait(&full[st.s], st.ph, abort_flag, c.budget))) break;
           mbar_arrive(&empty[st.s]);
           st.next(NS);
         }
@@ -544,7 +562,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         const Ring v = st;
         st.next(NS);
         if (j >= n) continue;
-        ok = mbar_wait(&s_full[t], n_s & 1, abort_flag);
+        ok = tc_wait(&s_full[t], n_s & 1, abort_flag, c.budget);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         tc_fence_after();
@@ -578,7 +596,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         // P and O are this warpgroup's once the product before has ended
         auto product_before = [&]() {
           if (n_s == 0) return true;
-          ok = mbar_wait(&pv_done[t], (n_s - 1) & 1, abort_flag);
+          ok = tc_wait(&pv_done[t], (n_s - 1) & 1, abort_flag, c.budget);
           ok = __all_sync(0xFFFFFFFFu, ok);
           tc_fence_after();
           return ok;
@@ -617,7 +635,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         if constexpr (BN % 32 != 0) tmem_st_x8(a_p + BN / 32 * 16, w + BN / 32 * 16);
         const int keys_here = it.s.nk - j * BN;
         if (keys_here < BN) {  // V rows behind the sequence: zeros
-          ok = mbar_wait(&full[v.s], v.ph, abort_flag);
+          ok = tc_wait(&full[v.s], v.ph, abort_flag, c.budget);
           ok = __all_sync(0xFFFFFFFFu, ok);
           if (!ok) break;
           uint8_t* vt = sKV + v.s * F::kKvBytes + keys_here * 128;
@@ -639,7 +657,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       uint16_t* yt = p.y + static_cast<int64_t>(it.s.q0 + it.row0 + t * kTcTile) * p.ldy + it.head * p.y_hs;
       float o[(F::D + 31) / 32 * 32];
       if (n > 0) {
-        ok = mbar_wait(&pv_done[t], (n_s - 1) & 1, abort_flag);
+        ok = tc_wait(&pv_done[t], (n_s - 1) & 1, abort_flag, c.budget);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         tc_fence_after();
@@ -727,6 +745,8 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   c.tiles = static_cast<int32_t>(tiles);
   c.items = static_cast<int32_t>(tiles * pairs);
   // Without a mask all items are alike and a pair's stand together, for its K and V in L2; with one, 64 pairs.
+  // Six items of the most keys there can be, at 8192 cycles a tile (2500 or so are usual), on top of the library's usual limit.
+  c.budget = kWaitBudgetCycles + 6 * 8192 * (p.Mk / 80 + 1);
   // Packed sequences are taken longest first, and only items that are there: 16 documents of 1 to 1500 tokens.
   c.sorted = !p.causal && p.q_start != nullptr && p.n_seq <= kTcSorted;
   const int64_t group = p.causal ? 64 : 1;

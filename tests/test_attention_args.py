@@ -44,6 +44,7 @@ def _call(a, q=A, ldq=256, Mq=20, k=2 * A, ldk=128, v=3 * A, ldv=128, Mk=40, y=4
     (B.DP_ERR_INVALID_ARG, dict(scale=-1.0), {}),
     (B.DP_ERR_INVALID_ARG, dict(cap=-1.0), {}),
     (B.DP_ERR_INVALID_ARG, dict(cap=float("inf")), {}),
+    (B.DP_ERR_INVALID_ARG, dict(cap=1e5), {}),
     (B.DP_ERR_SHAPE, {}, dict(ldq=56)),
     (B.DP_ERR_SHAPE, dict(k_head_stride=56), {}),
     (B.DP_ERR_SHAPE, dict(k_head_stride=-64), {}),

@@ -301,3 +301,26 @@ def test_output_in_columns_of_the_inputs_buffer(flags):
     want, tol = R.attention(*(t.reshape(n, H, D) for t in (q, k, v)), [n], [n], y.reshape(n, H, D), 0.125)
     assert ((y.reshape(n, H, D).double() - want).abs() <= tol).all()
     assert torch.equal(buf[:, :3 * W], before[:, :3 * W])
+
+
+@pytest.mark.parametrize("flags", [0, B.DP_FLAG_FORCE_MMA])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n_seq", [63, 64, 65, 150])
+def test_many_sequences_of_unlike_lengths(n_seq, causal, flags):
+    """More work items than SMs, sequences sorted by length up to 64 of them, empty ones among them."""
+    gen = torch.Generator().manual_seed(n_seq)
+    lens = torch.randint(0, 300, (n_seq,), generator=gen).tolist()
+    lens[n_seq // 2], lens[-1], lens[0] = 0, 700, 1
+    _run(4, 2, 40, lens, lens, causal=causal, flags=flags, pad=3, seed=n_seq)
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_many_rounds_of_equal_items(D):
+    _run(8, 8, D, [300] * 40, [300] * 40, fixed=True, seed=D)
+    _run(8, 4, D, [520] * 12, [520] * 12, fixed=True, causal=True, prefix=[0, 5, 130, 600] * 3, seed=D)
+
+
+def test_long_sequence():
+    """Tiles far behind each other, and one query among them."""
+    _run(1, 1, 64, [6000], [6000], fixed=True, causal=True, seed=1)
+    _run(2, 1, 128, [130], [30011], layout="rows", seed=2)
