@@ -128,9 +128,9 @@ __device__ __forceinline__ uint16_t* at_out(const AttnParams& p, const AttnSeq& 
   return p.y + static_cast<int64_t>(s.q0 + static_cast<int>(row / group)) * p.ldy + (kvh * group + static_cast<int>(row % group)) * p.y_hs;
 }
 
-// 16 MB rows by every warp, each with keys of its own. grid.x = splits * KV * n_seq, clusters of `splits` along x.
-template <int DP, int MB>
-__global__ void __launch_bounds__(kAtThreads)
+// 16 MB rows by every one of W warps, each with keys of its own. grid.x = splits * KV * n_seq, clusters of `splits` along x.
+template <int DP, int MB, int W>
+__global__ void __launch_bounds__(32 * W)
 attn_few_kernel(const AttnParams p, const int splits) {
   constexpr int ROWS = 16 * MB, RB = at_row_bytes(DP), KS = DP / 16, NB = DP / 8, OW = DP + 4;
   constexpr int STAGE = 2 * kFewKeys * RB, kFewStages = few_stages(DP);
@@ -150,7 +150,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
   const int64_t rows = static_cast<int64_t>(s.nq) * group;  // (at most 16 MB)
   if (rows == 0) return;  // (the whole cluster)
   const int keys = attn_keys(p, s, s.nq - 1);
-  const int n = (keys + kFewKeys - 1) / kFewKeys, parts = splits * 4, part_at = split * 4 + warp;
+  const int n = (keys + kFewKeys - 1) / kFewKeys, parts = splits * W, part_at = split * W + warp;
   const int begin = static_cast<int>(static_cast<int64_t>(n) * part_at / parts), end = static_cast<int>(static_cast<int64_t>(n) * (part_at + 1) / parts);
   const uint16_t* kp = p.k + static_cast<int64_t>(s.k0) * p.ldk + kvh * p.k_hs;
   const uint16_t* vp = p.v + static_cast<int64_t>(s.k0) * p.ldv + kvh * p.v_hs;
@@ -266,8 +266,8 @@ attn_few_kernel(const AttnParams p, const int splits) {
   }
   cp_async_wait<0>();
   __syncthreads();  // ---- join: the CTA's warps, then the cluster's CTAs ----
-  float* part = reinterpret_cast<float*>(at_smem);  // [4][ROWS][OW]: O, then m and l
-  float* joined = part + 4 * ROWS * OW;             // [ROWS][OW]
+  float* part = reinterpret_cast<float*>(at_smem);  // [W][ROWS][OW]: O, then m and l
+  float* joined = part + W * ROWS * OW;             // [ROWS][OW]
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
 #pragma unroll
@@ -281,13 +281,13 @@ attn_few_kernel(const AttnParams p, const int splits) {
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < static_cast<int>(rows) * (DP / 4); i += kAtThreads) {
+  for (int i = threadIdx.x; i < static_cast<int>(rows) * (DP / 4); i += 32 * W) {
     const int r = i / (DP / 4), c = i % (DP / 4);
     float mm = -INFINITY, ll = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) mm = fmaxf(mm, part[(k * ROWS + r) * OW + DP]);
+    for (int k = 0; k < W; ++k) mm = fmaxf(mm, part[(k * ROWS + r) * OW + DP]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < W; ++k) {
       const float* pr = part + (k * ROWS + r) * OW;
       const float f = mm == -INFINITY ? 0.0f : ex2(pr[DP] - mm);
       ll = fmaf(pr[DP + 1], f, ll);
@@ -307,7 +307,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
   if (splits == 1) return;
   __syncwarp();
   cluster_sync();
-  for (int i = threadIdx.x + kAtThreads * split; i < static_cast<int>(rows) * (DP / 2); i += kAtThreads * splits) {
+  for (int i = threadIdx.x + 32 * W * split; i < static_cast<int>(rows) * (DP / 2); i += 32 * W * splits) {
     const int r = i / (DP / 2), c = i % (DP / 2);
     if (2 * c >= p.D) continue;
     float pm[kAtMaxSplits], pl[kAtMaxSplits], a0[kAtMaxSplits], a1[kAtMaxSplits], mm = -INFINITY;
@@ -462,17 +462,24 @@ attn_rows_kernel(const AttnParams p, const int tiles) {
 // ---- host side -------------------------------------------------------------------------------------
 template <int DP>
 constexpr size_t at_rows_smem() { return static_cast<size_t>(kAtStages) * at_stage_bytes(DP); }
-template <int DP, int MB>
+template <int DP, int MB, int W>
 constexpr size_t at_few_smem() {
-  constexpr size_t ring = 4 * static_cast<size_t>(few_stages(DP)) * 2 * kFewKeys * at_row_bytes(DP);
-  constexpr size_t join = 5 * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
+  constexpr size_t ring = W * static_cast<size_t>(few_stages(DP)) * 2 * kFewKeys * at_row_bytes(DP);
+  constexpr size_t join = (W + 1) * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
   return ring > join ? ring : join;
+}
+template <int DP, int MB, int W>
+static cudaError_t at_few_init() {
+  return cudaFuncSetAttribute(attn_few_kernel<DP, MB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(at_few_smem<DP, MB, W>()));
 }
 template <int DP>
 static int at_init() {
   DP_CUDA_OK(cudaFuncSetAttribute(attn_rows_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(at_rows_smem<DP>())));
-  DP_CUDA_OK((cudaFuncSetAttribute(attn_few_kernel<DP, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(at_few_smem<DP, 1>()))));
-  DP_CUDA_OK((cudaFuncSetAttribute(attn_few_kernel<DP, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(at_few_smem<DP, 2>()))));
+  DP_CUDA_OK((at_few_init<DP, 1, 4>()));
+  DP_CUDA_OK((at_few_init<DP, 2, 4>()));
+  DP_CUDA_OK((at_few_init<DP, 1, 8>()));
+  DP_CUDA_OK((at_few_init<DP, 2, 8>()));
   return DP_OK;
 }
 int attn_init_device() {
@@ -484,13 +491,17 @@ int attn_init_device() {
   return st;
 }
 
+template <int DP, int MB, int W>
+static cudaError_t launch_few(const AttnParams& p, unsigned grid, int splits, cudaStream_t stream, bool pdl) {
+  return launch_cluster(attn_few_kernel<DP, MB, W>, dim3(grid), dim3(32 * W), at_few_smem<DP, MB, W>(), stream, pdl,
+                        static_cast<unsigned>(splits), p, splits);
+}
 template <int DP>
-static cudaError_t launch_at(const AttnParams& p, unsigned grid, int tiles, int splits, int64_t rows, cudaStream_t stream, bool pdl) {
-  const dim3 block(kAtThreads);
-  const unsigned cluster = static_cast<unsigned>(splits);
-  if (tiles > 0) return launch(attn_rows_kernel<DP>, dim3(grid), block, at_rows_smem<DP>(), stream, pdl, p, tiles);
-  if (rows <= 16) return launch_cluster(attn_few_kernel<DP, 1>, dim3(grid), block, at_few_smem<DP, 1>(), stream, pdl, cluster, p, splits);
-  return launch_cluster(attn_few_kernel<DP, 2>, dim3(grid), block, at_few_smem<DP, 2>(), stream, pdl, cluster, p, splits);
+static cudaError_t launch_at(const AttnParams& p, unsigned grid, int tiles, int splits, int warps, int64_t rows, cudaStream_t stream,
+                             bool pdl) {
+  if (tiles > 0) return launch(attn_rows_kernel<DP>, dim3(grid), dim3(kAtThreads), at_rows_smem<DP>(), stream, pdl, p, tiles);
+  return warps == 4 ? rows <= 16 ? launch_few<DP, 1, 4>(p, grid, splits, stream, pdl) : launch_few<DP, 2, 4>(p, grid, splits, stream, pdl)
+                    : rows <= 16 ? launch_few<DP, 1, 8>(p, grid, splits, stream, pdl) : launch_few<DP, 2, 8>(p, grid, splits, stream, pdl);
 }
 
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
@@ -500,21 +511,25 @@ int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const bool few = rows <= 32 && p.max_k > kAtKeys;
   const int64_t tiles = few ? 0 : (rows + 63) / 64;
   const int64_t units = (few ? 1 : tiles) * p.KV * p.n_seq;
-  int splits = 1;
-  if (few) {  // as many CTAs as the SMs hold, two each, as long as a warp has a tile of keys
-    const int64_t key_tiles = (static_cast<int64_t>(p.max_k) + kFewKeys - 1) / kFewKeys, most = 2 * num_sms() / units;
-    splits = static_cast<int>(key_tiles / 4 < most ? key_tiles / 4 : most);
+  int splits = 1, warps = 4;
+  if (few) {
+    // As many CTAs of four warps as the SMs hold, two each, up to eight to a (sequence, head) pair, as long as a warp has a tile of
+    // keys; of eight warps where there are only a few pairs. (4 pairs of 4 x 128, 8192 keys: 18.5 us by four warps, 15.4 by eight;
+    // 16 pairs of 72: 17.5 and 22, since clusters of eight whole SMs are hard to place.)
+    warps = units <= 8 ? 8 : 4;
+    const int64_t most = (warps == 8 ? 1 : 2) * num_sms() / units, tiles_of_keys = (static_cast<int64_t>(p.max_k) + kFewKeys - 1) / kFewKeys;
+    splits = static_cast<int>(tiles_of_keys / warps < most ? tiles_of_keys / warps : most);
     splits = splits < 1 ? 1 : splits > kAtMaxSplits ? kAtMaxSplits : splits;
   }
   if (units * splits > 0x7FFFFFFF || tiles > 0x7FFFFFFF)
     return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)units);
   const unsigned grid = static_cast<unsigned>(units * splits);
   const int t = static_cast<int>(tiles);
-  const cudaError_t e = p.D <= 32   ? launch_at<32>(p, grid, t, splits, rows, stream, pdl)
-                        : p.D <= 64 ? launch_at<64>(p, grid, t, splits, rows, stream, pdl)
-                        : p.D <= 80 ? launch_at<80>(p, grid, t, splits, rows, stream, pdl)
-                        : p.D <= 96 ? launch_at<96>(p, grid, t, splits, rows, stream, pdl)
-                                    : launch_at<128>(p, grid, t, splits, rows, stream, pdl);
+  const cudaError_t e = p.D <= 32   ? launch_at<32>(p, grid, t, splits, warps, rows, stream, pdl)
+                        : p.D <= 64 ? launch_at<64>(p, grid, t, splits, warps, rows, stream, pdl)
+                        : p.D <= 80 ? launch_at<80>(p, grid, t, splits, warps, rows, stream, pdl)
+                        : p.D <= 96 ? launch_at<96>(p, grid, t, splits, warps, rows, stream, pdl)
+                                    : launch_at<128>(p, grid, t, splits, warps, rows, stream, pdl);
   if (e != cudaSuccess) return fail(DP_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
   return DP_OK;
 }
