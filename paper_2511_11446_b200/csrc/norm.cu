@@ -23,7 +23,7 @@
 namespace dp {
 
 constexpr int kGnMaxChunks = 128, kGnMaxThreads = 640;
-constexpr int kGnUnroll = 4;                   // rows that a thread adds while as many are in flight
+constexpr int kGnSumUnroll = 6, kGnUnroll = 4;                  // rows that a thread adds while as many are in flight
 constexpr int kGnMaxCluster = 8;               // (16, measured: 8 samples of 64 x 640 12.7 us, 6.5 with 8)
 constexpr size_t kGnSmem = 113 * 1024;          // of a CTA: two to an SM, one of which reads while the other writes
 
@@ -34,6 +34,7 @@ struct GnArgs {
   uint64_t per_inv;    // ceil(2^32 / per): c / per = c * per_inv >> 32 for c < 2^16 (a division takes twenty instructions)
   const uint16_t *gamma, *beta;  // [C] or null
   float eps;
+  double inv_n;        // 1 / values of a group
   uint16_t* y;
   int64_t ldy;
   int8_t* q;
@@ -94,9 +95,9 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
     uint4* keep = rows_at + t.lane * t.vecs + t.vec;
     const int64_t step = t.lanes * a.ldx;
     const int keep_step = t.lanes * t.vecs;
-    uint4 v[kGnUnroll];
+    uint4 v[kGnSumUnroll];
 #pragma unroll
-    for (int u = 0; u < kGnUnroll; ++u, xp += step)
+    for (int u = 0; u < kGnSumUnroll; ++u, xp += step)
       if (u < n) v[u] = ld_global_v4(xp);
     uint64_t s2[4], ss2[4], minus[4];
 #pragma unroll
@@ -115,20 +116,20 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
       }
     };
     // the next rows are on their way while these are added
-    for (; n > 0; n -= kGnUnroll) {
-      uint4 nx[kGnUnroll];
+    for (; n > 0; n -= kGnSumUnroll) {
+      uint4 nx[kGnSumUnroll];
 #pragma unroll
-      for (int u = 0; u < kGnUnroll; ++u, xp += step)
-        if (u + kGnUnroll < n) nx[u] = ld_global_v4(xp);
+      for (int u = 0; u < kGnSumUnroll; ++u, xp += step)
+        if (u + kGnSumUnroll < n) nx[u] = ld_global_v4(xp);
 #pragma unroll
-      for (int u = 0; u < kGnUnroll; ++u)
+      for (int u = 0; u < kGnSumUnroll; ++u)
         if (u < n) {
           if constexpr (KEEP) keep[u * keep_step] = v[u];
           add(v[u]);
         }
-      if constexpr (KEEP) keep += kGnUnroll * keep_step;
+      if constexpr (KEEP) keep += kGnSumUnroll * keep_step;
 #pragma unroll
-      for (int u = 0; u < kGnUnroll; ++u) v[u] = nx[u];
+      for (int u = 0; u < kGnSumUnroll; ++u) v[u] = nx[u];
     }
     float s[8], ss[8];
 #pragma unroll
@@ -210,11 +211,13 @@ __device__ __forceinline__ void gn_groups(const GnArgs& a, const uint16_t* xs, i
       w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
     }
     if (live && k == 0) {
-      const double n = static_cast<double>(a.rows) * a.per, mean = u / n;
-      const double var = fmax(w / n - mean * mean, 0.0);
+      const double mean = u * a.inv_n, var = fmax(w * a.inv_n - mean * mean, 0.0);
+      const float v = static_cast<float>(var + static_cast<double>(a.eps));
+      float r = rsqrtf(v);
+      if (v > 1e-30f) r = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);  // (a step of Newton's: the last bits; none where v r^2 would underflow)
       out[3 * g] = gn_bf16(xs + g * a.per);
       out[3 * g + 1] = static_cast<float>(mean);
-      out[3 * g + 2] = static_cast<float>(1.0 / sqrt(var + static_cast<double>(a.eps)));
+      out[3 * g + 2] = r;
     }
   }
 }
@@ -522,7 +525,7 @@ int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, i
                       const void* beta, float eps, bool silu, void* y, int64_t ldy, int8_t* q, int64_t ldq, float* s_a,
                       void* workspace, cudaStream_t stream) {
   GnArgs a{static_cast<const uint16_t*>(x), rows, ldx, C, G, C / G, ((1ull << 32) + C / G - 1) / (C / G), static_cast<const uint16_t*>(gamma),
-           static_cast<const uint16_t*>(beta), eps, static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
+           static_cast<const uint16_t*>(beta), eps, 1.0 / (static_cast<double>(rows) * (C / G)), static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
            static_cast<float2*>(workspace), 0, 0};
   const bool codes = q != nullptr;
   const int threads = gn_threads(C);
