@@ -29,7 +29,7 @@ namespace dp {
 
 constexpr int kTcTile = 128;                      // queries of a tile
 constexpr int kTcBlock = kTcTile * 128;           // bytes of 128 rows x 64 columns
-constexpr int kTcThreads = 384;                   // two warpgroups; loads, an issuing warp for each tile, one idle
+constexpr int kTcThreads = 384;                   // two warpgroups; loads, an issuing warp for each tile, work items
 // Registers a thread: 384 threads are launched with 168; the third warpgroup gives up what the first two take on:
 // 2 * 128 * 208 + 128 * 88 = 384 * 168.
 constexpr int kTcRegsLaunch = 168, kTcRegsSoftmax = 208, kTcRegsRest = 88;
@@ -311,28 +311,53 @@ __device__ __forceinline__ void tc_sort(const AttnParams& p, const AttnTcSched& 
   if (lane == 0) o.start[kTcSorted] = before;
   __syncwarp();
 }
+// Item i in the order without a sort: pairs in groups; within a group the last rows, which see the most keys under a causal mask, come
+// first. The sequence.
+__device__ __forceinline__ int tc_place(const AttnParams& p, const AttnTcSched& c, int i, int& head, int& tile) {
+  const int pairs = p.H * p.n_seq, g = i / (c.group * c.tiles), in = i - g * c.group * c.tiles;
+  const int size = min(c.group, pairs - g * c.group), from_last = in / size;
+  const int pair = g * c.group + in - from_last * size, seq = pair / p.H;
+  head = pair - seq * p.H;
+  tile = c.tiles - 1 - from_last;
+  return seq;
+}
 // The next item of this CTA: rounds of gridDim.x items, every other one backwards, so that the long items that come first
-// even out. `rank`: where the last one was found. False: there is none.
+// even out. `rank`: where the last one was found. False: there is none. By a whole warp: where packed sequences are shorter than
+// max_q most items may not be there, and the lanes look through 32 rounds at a time (256 sequences of 200 tokens, 16 heads of 72,
+// causal, max_q = 8192: 395 us by one thread, 201 so).
 template <int BN>
 __device__ __forceinline__ bool tc_next(const AttnParams& p, const AttnTcSched& c, const TcOrder& o, int& round, int& rank, TcItem& it) {
   const int items = c.sorted ? o.start[kTcSorted] : c.items;
+  auto at = [&](int r) {
+    return static_cast<int64_t>(r) * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+  };
   for (;;) {
-    const int64_t base = static_cast<int64_t>(round) * gridDim.x;
-    if (base >= items) return false;
-    const int64_t at = base + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    ++round;
-    if (at >= items) continue;
-    const int i = static_cast<int>(at);
+    if (static_cast<int64_t>(round) * gridDim.x >= items) return false;
+    const int64_t here = at(round++);
+    int head, tile;
+    if (here >= items) continue;
+    const int i = static_cast<int>(here);
     if (c.sorted) {  // (items of later rounds stand behind those of earlier ones)
       while (o.start[rank + 1] <= i) ++rank;
-      const int in = i - o.start[rank], tile = in / p.H;
+      const int in = i - o.start[rank];
+      tile = in / p.H;
       if (tc_item<BN>(p, c, o.seq[rank], in - tile * p.H, tile, it)) return true;
-    } else {
-      // pairs in groups; within a group the last rows, which see the most keys under a causal mask, come first
-      const int pairs = p.H * p.n_seq, g = i / (c.group * c.tiles), in = i - g * c.group * c.tiles;
-      const int size = min(c.group, pairs - g * c.group), from_last = in / size;
-      const int pair = g * c.group + in - from_last * size, seq = pair / p.H;
-      if (tc_item<BN>(p, c, seq, pair - seq * p.H, c.tiles - 1 - from_last, it)) return true;
+      continue;
+    }
+    const int seq = tc_place(p, c, i, head, tile);
+    if (tc_item<BN>(p, c, seq, head, tile, it)) return true;
+    for (;; round += 32) {
+      if (static_cast<int64_t>(round) * gridDim.x >= items) return false;
+      const int64_t mine = at(round + static_cast<int>(threadIdx.x & 31));
+      bool there = false;
+      if (mine < items) {
+        const int s = tc_place(p, c, static_cast<int>(mine), head, tile);
+        there = static_cast<int64_t>(tile) * c.rows < attn_seq(p, s).nq;
+      }
+      if (const uint32_t some = __ballot_sync(0xFFFFFFFFu, there); some != 0) {
+        round += __ffs(some) - 1;
+        break;
+      }
     }
   }
 }
@@ -453,16 +478,19 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       int round = 0, rank = 0;
       if (c.sorted) tc_sort(p, c, *order);
       TcItem it;
-      if (elect_one()) {
-        bool ok = true, more = true;
-        while (ok && more) {
-          more = tc_next<BN>(p, c, *order, round, rank, it);
-          if (!more) it.row0 = -1;
-          if (!(ok = tc_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag, c.budget))) break;
-          slots[item_at.s] = it;
-          mbar_arrive(&item_full[item_at.s]);
-          item_at.next(kTcSlots);
+      bool ok = true, more = true;
+      while (ok && more) {
+        more = tc_next<BN>(p, c, *order, round, rank, it);
+        if (!more) it.row0 = -1;
+        if (lane == 0) {
+          ok = tc_wait(&item_empty[item_at.s], item_at.ph ^ 1u, abort_flag, c.budget);
+          if (ok) {
+            slots[item_at.s] = it;
+            mbar_arrive(&item_full[item_at.s]);
+          }
         }
+        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
+        item_at.next(kTcSlots);
       }
     } else if ((warp == 9 || warp == 10) && elect_one()) {
       // ================= products of tile t =================
@@ -744,14 +772,17 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   if (tiles * pairs > 0x7FFFFFFF) return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)(tiles * pairs));
   c.tiles = static_cast<int32_t>(tiles);
   c.items = static_cast<int32_t>(tiles * pairs);
-  // Without a mask all items are alike and a pair's stand together, for its K and V in L2; with one, 64 pairs.
-  // Six items of the most keys there can be, at 8192 cycles a tile (2500 or so are usual), on top of the library's usual limit.
-  c.budget = kWaitBudgetCycles + 6 * 8192 * (p.Mk / 80 + 1);
+  // Of equal sequences without a mask all items are alike and a pair's stand together, for its K and V in L2; else 64 pairs, so that
+  // what is there of a tile is a run of items (256 sequences of 200 tokens, 16 heads of 72, max_q = 1024: a pair's together 340 us,
+  // 64 pairs 186).
   // Packed sequences are taken longest first, and only items that are there: 16 documents of 1 to 1500 tokens.
   c.sorted = !p.causal && p.q_start != nullptr && p.n_seq <= kTcSorted;
-  const int64_t group = p.causal ? 64 : 1;
+  const int64_t group = p.causal || p.q_start != nullptr ? 64 : 1;
   c.group = static_cast<int32_t>(group < pairs ? group : pairs);
   const unsigned ctas = static_cast<unsigned>(c.items < sms ? c.items : sms);
+  // Six items of the most keys there can be, at 8192 cycles a tile (2500 or so are usual), and the items that may not be there,
+  // 4096 cycles (800) to 32 of them, on top of the library's usual limit.
+  c.budget = kWaitBudgetCycles + 6 * 8192 * (p.Mk / 80 + 1) + 4096 * (c.items / (32ll * ctas) + 1);
   return p.D <= 64   ? launch_tc<4>(p, c, ctas, stream, pdl)
          : p.D <= 80 ? launch_tc<5>(p, c, ctas, stream, pdl)
          : p.D <= 96 ? launch_tc<6>(p, c, ctas, stream, pdl)

@@ -314,6 +314,24 @@ def test_many_sequences_of_unlike_lengths(n_seq, causal, flags):
     _run(4, 2, 40, lens, lens, causal=causal, flags=flags, pad=3, seed=n_seq)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+def test_max_q_far_above_the_sequences(causal):
+    """max_q and max_k of a longest sequence that is not in this batch: nearly all tiles of queries are not there."""
+    n_seq, H, D = 2000, 4, 64
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    lens = [(7 * i) % 4 for i in range(n_seq)]
+    lens[3], lens[1500] = 700, 0
+    M = sum(lens)
+    q, k, v, y = (torch.randn(M, H * D, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(4))
+    starts, st = _starts(lens), torch.zeros(1, dtype=torch.int32, device="cuda")
+    at = B.make_attn(H, H, D, n_seq, 1 << 25, 1 << 25, 0.125, q_start=starts, k_start=starts, mask=int(causal))
+    B.dp_attention(at, q, H * D, M, k, H * D, v, H * D, M, y, H * D, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    want, tol = R.attention(*(t.view(M, H, D) for t in (q, k, v)), lens, lens, y.view(M, H, D), 0.125, 0.0, None, causal)
+    assert ((y.view(M, H, D).double() - want).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("D", [64, 72, 128])
 def test_many_rounds_of_equal_items(D):
     _run(8, 8, D, [300] * 40, [300] * 40, fixed=True, seed=D)
