@@ -568,6 +568,9 @@ static bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
 }
+// Whether `rows` rows `ld` elements apart end within 2^46 elements of their start: beyond every address space, and a product that
+// passes 64 bits would hide an overlap.
+static bool extent_ok(int64_t rows, int64_t ld) { return rows < 2 || ld <= (1ll << 46) / (rows - 1); }
 // `rows` x `heads` vectors of D elements of 16 bits.
 struct AttnRange {
   const void* p;
@@ -616,6 +619,9 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   constexpr int64_t kMaxStride = 1ll << 38;  // elements: a tensor map's strides stay below 2^40 bytes
   for (int64_t s : {ldq, ldk, ldv, ldy, qh, kh, vh, yh})
     if (s < D || s > kMaxStride) return fail(DP_ERR_SHAPE, "dp_attention: a stride of %lld elements for vectors of %d", (long long)s, D);
+  if (!extent_ok(Mq, ldq) || !extent_ok(Mq, ldy) || !extent_ok(Mk, ldk) || !extent_ok(Mk, ldv) || !extent_ok(H, qh) ||
+      !extent_ok(H, yh) || !extent_ok(KV, kh) || !extent_ok(KV, vh))
+    return fail(DP_ERR_SHAPE, "dp_attention: rows times strides beyond the address space");
   if (a->n_seq == 0 || a->max_q == 0 || Mq == 0) return DP_OK;
   if (H > 1 && ldy < (H - 1) * yh + D && yh < (Mq - 1) * ldy + D)
     return fail(DP_ERR_SHAPE, "dp_attention: heads and rows of y overlap");
@@ -677,7 +683,8 @@ static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, 
   if (act != DP_ACT_NONE && act != DP_ACT_SILU) return fail(DP_ERR_INVALID_ARG, "%s: act=%d", name, act);
   if (n == 0 || rows == 0) return DP_OK;
   if (!x || !out || (out_size == 1 && !s_a)) return fail(DP_ERR_INVALID_ARG, "%s: NULL argument", name);
-  if (ldx < C || ldo < C) return fail(DP_ERR_SHAPE, "%s: leading dimension smaller than the row", name);
+  if (ldx < C || ldo < C || !extent_ok(n * rows, ldx) || !extent_ok(n * rows, ldo))
+    return fail(DP_ERR_SHAPE, "%s: leading dimension smaller than the row, or beyond the address space", name);
   if (!aligned16(x) || !aligned16(out) || (ldx % 8) || (ldo * out_size % 16) || !aligned16(gamma) || !aligned16(beta) ||
       (reinterpret_cast<uintptr_t>(s_a) & 3u))
     return fail(DP_ERR_ALIGN, "%s: pointers and pitches must be 16-byte aligned", name);

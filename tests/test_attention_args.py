@@ -71,6 +71,22 @@ def test_attention_refusals(want, fields, args):
     assert B.lib().dp_last_error()
 
 
+@pytest.mark.parametrize("fields,args", [
+    ({}, dict(Mq=1 << 30, ldq=1 << 37)), ({}, dict(Mq=1 << 30, ldy=1 << 37)), ({}, dict(Mk=1 << 30, ldk=1 << 37)),
+    ({}, dict(Mk=1 << 30, ldv=1 << 37)), (dict(heads=1 << 20, kv_heads=1, q_head_stride=1 << 37), {}),
+    (dict(heads=1 << 20, kv_heads=1, y_head_stride=1 << 37), {}), (dict(heads=1 << 20, kv_heads=1 << 20, k_head_stride=1 << 37), {}),
+    (dict(heads=1 << 20, kv_heads=1 << 20, v_head_stride=1 << 37), {}),
+])
+def test_attention_buffers_beyond_any_address_space(fields, args):
+    """(their lengths in bytes do not fit 64 bits, where an overlap could go unseen)"""
+    assert _call(_attn(**fields), **args) == B.DP_ERR_SHAPE
+
+
+@pytest.mark.parametrize("kw", [dict(ldx=1 << 60), dict(ldo=1 << 60)])
+def test_group_norm_buffers_beyond_any_address_space(kw):
+    assert _gn(False, **kw) == B.DP_ERR_SHAPE and _gn(True, **kw) == B.DP_ERR_SHAPE
+
+
 def test_attention_nothing_to_do():
     assert _call(None) == B.DP_ERR_INVALID_ARG
     assert _call(_attn(n_seq=0), q=None, k=None, v=None, y=None) == B.DP_OK
