@@ -5,7 +5,7 @@
 //
 // A row is a (query, head) pair: the heads / kv_heads heads that read one key head stand beside each other, so keys and values
 // are read once for all of them. Few rows make this a stream of K and V (one query, 16 heads of 72: 4 operations a byte), so what
-// counts is bytes in flight: in attn_few_kernel every warp walks a part of the keys of its own, 32 at a time through a private ring
+// counts is bytes in flight: in attn_few_kernel every warp walks a part of the keys of its own, 16 or 32 at a time through a private ring
 // of cp.async stages without a barrier between warps, and the keys of a sequence are cut over the CTAs of a cluster too, whose
 // partial sums (m, l, O) meet in distributed shared memory: one launch, no scratch memory.
 #include <cuda_bf16.h>
@@ -17,9 +17,11 @@ namespace dp {
 
 constexpr int kAtThreads = 128, kAtKeys = 64;
 constexpr int kAtMaxSplits = 8;  // CTAs of a cluster
-constexpr int kFewKeys = 32;  // of a stage of a warp's ring
-// Stages of that ring: two CTAs to an SM (45 to 90 KB each).
-__host__ __device__ constexpr int few_stages(int dp) { return dp <= 96 ? 2 : 1; }
+// Keys of a stage of a warp's ring, and stages: two CTAs to an SM. Small stages cost more arithmetic a key, so they are taken only where they
+// overlap what else would wait (8 sequences of 8192 keys, 4 key heads of 128, one query: 32.9 us by one stage of 32, 28.2 by three of 16; seven
+// queries, two blocks of rows: 44.4 / 45.3).
+__host__ __device__ constexpr int few_keys(int dp, int mb) { return dp > 96 && mb == 1 ? 16 : 32; }
+__host__ __device__ constexpr int few_stages(int dp, int mb) { return dp <= 96 ? 2 : mb == 1 ? 3 : 1; }
 
 // Bytes between the rows of a tile in shared memory: an odd number of 16-byte units, so that the eight rows of a matrix that
 // ldmatrix fetches lie in different banks.
@@ -55,7 +57,7 @@ __device__ __forceinline__ void ld_cluster_f32x2(uint32_t a, float& x, float& y)
 }
 
 struct AtRows {
-  int tok[2], pos[2];  // of fragment rows lane / 4 and lane / 4 + 8 (tok < 0: none)
+  int pos[2];          // of fragment rows lane / 4 and lane / 4 + 8
   int bound[2];        // keys below it are visible
   float slope[2];
 };
@@ -99,22 +101,28 @@ __device__ __forceinline__ void at_scores(const AttnParams& p, const AtRows& w, 
     mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xFFFFFFFFu, mx[e], 2));
   }
 }
-// Rows row0 .. row0 + 15 of `rows` (a query's `group` heads side by side): their places and query fragments.
+// Where a CTA's rows lie (a query's `group` heads side by side): its first row is head `head0` of the group of query `tok0`, `left` rows
+// are there. (32-bit divisions row by row: 64-bit ones took 0.4 us of a small call's 6.2.)
+struct AtPlace {
+  int tok0, head0, left, group, kvh;
+  __device__ __forceinline__ int tok(int row) const { return tok0 + (head0 + row) / group; }
+  __device__ __forceinline__ int head(int row) const { return kvh * group + (head0 + row) % group; }
+};
+// Rows row0 .. row0 + 15 of the CTA: their places and query fragments.
 template <int KS>
-__device__ __forceinline__ void at_rows(const AttnParams& p, const AttnSeq& s, int kvh, int group, int64_t row0, int64_t rows,
-                                        AtRows& w, uint32_t (&qf)[KS][4]) {
+__device__ __forceinline__ void at_rows(const AttnParams& p, const AttnSeq& s, const AtPlace& at, int row0, AtRows& w,
+                                        uint32_t (&qf)[KS][4]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const int64_t row = row0 + (lane >> 2) + 8 * e;
-    const bool live = row < rows;
-    w.tok[e] = live ? static_cast<int>(row / group) : -1;
-    const int head = kvh * group + (live ? static_cast<int>(row % group) : 0);
-    w.pos[e] = w.tok[e] + s.behind;
+    const int row = row0 + (lane >> 2) + 8 * e;
+    const bool live = row < at.left;
+    const int tok = live ? at.tok(row) : 0, head = live ? at.head(row) : at.kvh * at.group;
+    w.pos[e] = tok + s.behind;
     w.bound[e] = p.causal ? min(s.nk, max(w.pos[e] + 1, s.prefix)) : s.nk;
     if (!live) w.bound[e] = 0x7FFFFFFF;  // (nobody's row: nothing to be masked)
     w.slope[e] = p.slopes != nullptr ? ld_global_f32(p.slopes + head) * kLog2e : 0.0f;
-    const uint16_t* qr = p.q + static_cast<int64_t>(s.q0 + (live ? w.tok[e] : 0)) * p.ldq + head * p.q_hs;
+    const uint16_t* qr = p.q + static_cast<int64_t>(s.q0 + tok) * p.ldq + head * p.q_hs;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -124,8 +132,8 @@ __device__ __forceinline__ void at_rows(const AttnParams& p, const AttnSeq& s, i
       }
   }
 }
-__device__ __forceinline__ uint16_t* at_out(const AttnParams& p, const AttnSeq& s, int kvh, int group, int64_t row) {
-  return p.y + static_cast<int64_t>(s.q0 + static_cast<int>(row / group)) * p.ldy + (kvh * group + static_cast<int>(row % group)) * p.y_hs;
+__device__ __forceinline__ uint16_t* at_out(const AttnParams& p, const AttnSeq& s, const AtPlace& at, int row) {
+  return p.y + static_cast<int64_t>(s.q0 + at.tok(row)) * p.ldy + at.head(row) * p.y_hs;
 }
 
 // 16 MB rows by every one of W warps, each with keys of its own. grid.x = splits * KV * n_seq, clusters of `splits` along x.
@@ -133,7 +141,8 @@ template <int DP, int MB, int W>
 __global__ void __launch_bounds__(32 * W)
 attn_few_kernel(const AttnParams p, const int splits) {
   constexpr int ROWS = 16 * MB, RB = at_row_bytes(DP), KS = DP / 16, NB = DP / 8, OW = DP + 4;
-  constexpr int STAGE = 2 * kFewKeys * RB, kFewStages = few_stages(DP);
+  constexpr int STAGE = 2 * few_keys(DP, MB) * RB;
+  constexpr int kFewKeys = few_keys(DP, MB), kFewStages = few_stages(DP, MB);
   extern __shared__ __align__(128) uint8_t at_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
@@ -147,8 +156,9 @@ attn_few_kernel(const AttnParams p, const int splits) {
     }
   pdl_wait();
   const AttnSeq s = attn_seq(p, u / p.KV);
-  const int64_t rows = static_cast<int64_t>(s.nq) * group;  // (at most 16 MB)
+  const int rows = s.nq * group;  // (at most 16 MB)
   if (rows == 0) return;  // (the whole cluster)
+  const AtPlace at{0, 0, rows, group, kvh};
   const int keys = attn_keys(p, s, s.nq - 1);
   const int n = (keys + kFewKeys - 1) / kFewKeys, parts = splits * W, part_at = split * W + warp;
   const int begin = static_cast<int>(static_cast<int64_t>(n) * part_at / parts), end = static_cast<int>(static_cast<int64_t>(n) * (part_at + 1) / parts);
@@ -170,7 +180,8 @@ attn_few_kernel(const AttnParams p, const int splits) {
     const int left = keys - t * kFewKeys;  // keys of this tile
     // rows behind the sequence belong to others: zeros in their place (and the first key's address, which exists)
 #pragma unroll 2
-    for (int i = 0; i < vecs * kFewKeys / 32; ++i) {
+    for (int i = 0; i < (vecs * kFewKeys + 31) / 32; ++i) {
+      if (kFewKeys % 32 != 0 && r >= kFewKeys) break;
       const bool ok = r < left;
       cp_async_16(dst, ok ? ks : kp, ok);
       cp_async_16(dst + kFewKeys * RB, ok ? vs : vp, ok);
@@ -193,7 +204,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
   float o[MB][NB][4], m[MB][2], l[MB][2];
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    at_rows<KS>(p, s, kvh, group, 16 * b, rows, w[b], qf[b]);
+    at_rows<KS>(p, s, at, 16 * b, w[b], qf[b]);
 #pragma unroll
     for (int k = 0; k < NB; ++k) o[b][k][0] = o[b][k][1] = o[b][k][2] = o[b][k][3] = 0.0f;
     m[b][0] = m[b][1] = -INFINITY;
@@ -281,7 +292,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < static_cast<int>(rows) * (DP / 4); i += 32 * W) {
+  for (int i = threadIdx.x; i < rows * (DP / 4); i += 32 * W) {
     const int r = i / (DP / 4), c = i % (DP / 4);
     float mm = -INFINITY, ll = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -297,7 +308,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
     if (splits == 1) {
       const float inv = ll != 0.0f ? __fdiv_rn(1.0f, ll) : 0.0f;  // (no key in sight: O is zero too)
       if (4 * c < p.D)
-        *reinterpret_cast<uint2*>(at_out(p, s, kvh, group, r) + 4 * c) =
+        *reinterpret_cast<uint2*>(at_out(p, s, at, r) + 4 * c) =
             make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
     } else {
       *reinterpret_cast<float4*>(joined + r * OW + 4 * c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -307,7 +318,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
   if (splits == 1) return;
   __syncwarp();
   cluster_sync();
-  for (int i = threadIdx.x + 32 * W * split; i < static_cast<int>(rows) * (DP / 2); i += 32 * W * splits) {
+  for (int i = threadIdx.x + 32 * W * split; i < rows * (DP / 2); i += 32 * W * splits) {
     const int r = i / (DP / 2), c = i % (DP / 2);
     if (2 * c >= p.D) continue;
     float pm[kAtMaxSplits], pl[kAtMaxSplits], a0[kAtMaxSplits], a1[kAtMaxSplits], mm = -INFINITY;
@@ -331,7 +342,7 @@ attn_few_kernel(const AttnParams p, const int splits) {
         x1 = fmaf(a1[k], f, x1);
       }
     const float inv = ll != 0.0f ? __fdiv_rn(1.0f, ll) : 0.0f;
-    *reinterpret_cast<uint32_t*>(at_out(p, s, kvh, group, r) + 2 * c) = pack_bf16(x0 * inv, x1 * inv);
+    *reinterpret_cast<uint32_t*>(at_out(p, s, at, r) + 2 * c) = pack_bf16(x0 * inv, x1 * inv);
   }
   __syncwarp();
   cluster_sync();  // nobody leaves while its partial sums are read
@@ -359,7 +370,9 @@ attn_rows_kernel(const AttnParams p, const int tiles) {
   const int64_t rows = static_cast<int64_t>(s.nq) * group;
   const int64_t row0 = static_cast<int64_t>(tile) * ROWS;
   if (row0 >= rows) return;
-  const int keys = attn_keys(p, s, static_cast<int>(min(row0 + ROWS, rows) - 1) / group);
+  const int tok0 = static_cast<int>(row0 / group);
+  const AtPlace at{tok0, static_cast<int>(row0 - static_cast<int64_t>(tok0) * group), static_cast<int>(min(rows - row0, static_cast<int64_t>(ROWS))), group, kvh};
+  const int keys = attn_keys(p, s, at.tok(at.left - 1));
   const int n_tiles = (keys + kAtKeys - 1) / kAtKeys;
   const uint16_t* kp = p.k + static_cast<int64_t>(s.k0) * p.ldk + kvh * p.k_hs;
   const uint16_t* vp = p.v + static_cast<int64_t>(s.k0) * p.ldv + kvh * p.v_hs;
@@ -383,7 +396,7 @@ attn_rows_kernel(const AttnParams p, const int tiles) {
   }
   AtRows w;
   uint32_t qf[KS][4];
-  at_rows<KS>(p, s, kvh, group, row0 + warp * 16, rows, w, qf);
+  at_rows<KS>(p, s, at, warp * 16, w, qf);
   float o[NB][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int k = 0; k < NB; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.0f;
@@ -447,9 +460,9 @@ attn_rows_kernel(const AttnParams p, const int tiles) {
   for (int e = 0; e < 2; ++e) {
     l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 1);
     l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], 2);
-    const int64_t row = row0 + warp * 16 + (lane >> 2) + 8 * e;
-    if (row >= rows) continue;
-    uint16_t* yr = at_out(p, s, kvh, group, row);
+    const int row = warp * 16 + (lane >> 2) + 8 * e;
+    if (row >= at.left) continue;
+    uint16_t* yr = at_out(p, s, at, row);
     const float inv = l[e] != 0.0f ? __fdiv_rn(1.0f, l[e]) : 0.0f;  // (no key in sight: O is zero too)
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
@@ -464,7 +477,7 @@ template <int DP>
 constexpr size_t at_rows_smem() { return static_cast<size_t>(kAtStages) * at_stage_bytes(DP); }
 template <int DP, int MB, int W>
 constexpr size_t at_few_smem() {
-  constexpr size_t ring = W * static_cast<size_t>(few_stages(DP)) * 2 * kFewKeys * at_row_bytes(DP);
+  constexpr size_t ring = W * static_cast<size_t>(few_stages(DP, MB)) * 2 * few_keys(DP, MB) * at_row_bytes(DP);
   constexpr size_t join = (W + 1) * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
   return ring > join ? ring : join;
 }
@@ -517,7 +530,7 @@ int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
     // keys; of eight warps where there are only a few pairs. (4 pairs of 4 x 128, 8192 keys: 18.5 us by four warps, 15.4 by eight;
     // 16 pairs of 72: 17.5 and 22, since clusters of eight whole SMs are hard to place.)
     warps = units <= 8 ? 8 : 4;
-    const int64_t most = (warps == 8 ? 1 : 2) * num_sms() / units, tiles_of_keys = (static_cast<int64_t>(p.max_k) + kFewKeys - 1) / kFewKeys;
+    const int64_t most = (warps == 8 ? 1 : 2) * num_sms() / units, tiles_of_keys = (static_cast<int64_t>(p.max_k) + 31) / 32;
     splits = static_cast<int>(tiles_of_keys / warps < most ? tiles_of_keys / warps : most);
     splits = splits < 1 ? 1 : splits > kAtMaxSplits ? kAtMaxSplits : splits;
   }
