@@ -301,7 +301,8 @@ typedef struct dp_attn {
  * (columns of one qkv buffer: q, k, v point into it with the same ld). Pointers 16-byte aligned, strides multiples of 8 and
  * at least head_dim; y overlaps neither an input nor itself. Fewer than 2^31 - 1024 rows. flags: DP_FLAG_NO_PDL,
  * DP_FLAG_FORCE_SIMT (the kernel for few queries, whatever max_q is), DP_FLAG_FORCE_MMA (the tcgen05 kernel). No scratch
- * memory, nothing kept between calls; results do not depend on what runs beside the call. Enqueues one kernel. Errors:
+ * memory, nothing kept between calls; results do not depend on what runs beside the call. Buffers and stream belong to the
+ * current device. Enqueues one kernel. Errors:
  * DP_ERR_INVALID_ARG, DP_ERR_SHAPE, DP_ERR_ALIGN, DP_ERR_ARCH.
  */
 int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const void* k, int64_t ldk, const void* v,
@@ -322,7 +323,8 @@ int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const
  *   workspace   : >= dp_group_norm_workspace(...) bytes, 256-byte aligned, contents undefined before and after; one call at a
  *                 time may use it
  * C a multiple of 8, at most 4608, and of `groups` (at most 1024); x and the output 16-byte aligned, ldx and ldy multiples of
- * 8, ldq of 16; the output does not overlap x; at most 2^31 rows and 2^23 samples. n_samples == 0 or rows == 0 is a no-op.
+ * 8, ldq of 16; the output does not overlap x; at most 2^31 rows and 2^23 samples. Buffers and stream belong to the current device.
+ * Sums of squares have to stay in fp32's range; with eps = 0 a constant group gives NaN (0 / 0). n_samples == 0 or rows == 0 is a no-op.
  * Errors: DP_ERR_INVALID_ARG, DP_ERR_SHAPE, DP_ERR_ALIGN, DP_ERR_WORKSPACE, DP_ERR_ARCH.
  */
 #define DP_ACT_NONE 0

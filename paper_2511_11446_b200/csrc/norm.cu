@@ -9,7 +9,7 @@
 //
 // Statistics first: sums of d and d^2, d = x - pivot with the group's first value as pivot, so that a level far above the spread
 // does not cancel (a constant map gives var = 0 and h = beta exactly). A thread keeps 8 channels of every `lanes`-th row, in fp32
-// over at most a few thousand values; groups' sums of CTAs are added in double, in a fixed order, and give each channel
+// over a few hundred values (65536 for a batch of 100 GB); groups' sums of CTAs are added in double, in a fixed order, and give each channel
 //     h = (x - pivot) * a + b,   a = gamma * rstd,   b = beta - (mean - pivot) * a       (x - pivot is exact or nearly so)
 //
 // Bound by memory: 2 bytes in and 2 (or 1) out per element, if x need not be read twice from it. Two forms:
