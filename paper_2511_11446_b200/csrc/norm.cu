@@ -22,7 +22,7 @@
 
 namespace dp {
 
-constexpr int kGnMaxChunks = 128, kGnMaxThreads = 640;
+constexpr int kGnMaxThreads = 640;
 constexpr int kGnSumUnroll = 6, kGnUnroll = 4;                  // rows that a thread adds while as many are in flight
 constexpr int kGnMaxCluster = 8;               // (16, measured: 8 samples of 64 x 640 12.7 us, 6.5 with 8)
 constexpr size_t kGnSmem = 113 * 1024;          // of a CTA: two to an SM, one of which reads while the other writes
@@ -43,6 +43,8 @@ struct GnArgs {
   float2* sums;  // [sample][chunk][G]
   int32_t chunks;      // (CTAs of the cluster in the one-kernel form)
   int64_t chunk_rows;
+  int32_t out_chunks;  // of the kernel that applies them
+  int64_t out_rows;
 };
 
 __device__ __forceinline__ float gn_bf16(const uint16_t* p) {
@@ -437,11 +439,11 @@ __global__ void __launch_bounds__(kGnMaxThreads) gn_apply_kernel(const GnArgs a)
   pdl_launch_dependents();
   const GnThread t(a.C);
   // the last chunks first: of maps beyond the L2 they are what is left there
-  const int block = gridDim.x - 1 - blockIdx.x, sample = block / a.chunks, chunk = block % a.chunks;
-  const int64_t r0 = chunk * a.chunk_rows, m0 = sample * a.rows;
+  const int block = gridDim.x - 1 - blockIdx.x, sample = block / a.out_chunks, chunk = block % a.out_chunks;
+  const int64_t r0 = chunk * a.out_rows, m0 = sample * a.rows;
   const uint16_t* xs = a.x + m0 * a.ldx;
   pdl_wait();
-  gn_out<CODES, SILU>(a, t, gn_smem, gn_scales(a), m0, r0, min(r0 + a.chunk_rows, a.rows), GnFromGlobal{xs, a.ldx}, [&]() {
+  gn_out<CODES, SILU>(a, t, gn_smem, gn_scales(a), m0, r0, min(r0 + a.out_rows, a.rows), GnFromGlobal{xs, a.ldx}, [&]() {
     gn_groups(a, xs, a.chunks, gn_smem, [&](int c, int g) {
       float2 v;
       const float2* p = a.sums + (static_cast<int64_t>(sample) * a.chunks + c) * a.G + g;
@@ -483,32 +485,30 @@ __global__ void __launch_bounds__(kGnMaxThreads) gn_cluster_kernel(const GnArgs 
 }
 
 // ---- host side -------------------------------------------------------------------------------------
-static int gn_threads(int32_t C) {  // whole rows of C / 8 vectors
-  const int vecs = C / 8;
-  return (kGnMaxThreads / vecs * vecs + 31) / 32 * 32;
+static int gn_threads(int32_t C, int most = kGnMaxThreads) {  // whole rows of C / 8 vectors
+  const int vecs = C / 8, rows = most / vecs;
+  return ((rows < 1 ? 1 : rows) * vecs + 31) / 32 * 32;
 }
 static size_t gn_part_bytes(int32_t C) { return 2 * sizeof(float) * static_cast<size_t>(gn_threads(C) / (C / 8)) * C; }
-static int gn_head_bytes(int32_t C, int32_t G) { return static_cast<int>(sizeof(float)) * gn_head_floats(G, gn_threads(C) / (C / 8)); }
+static int gn_head_bytes(int32_t C, int32_t G, int threads) { return static_cast<int>(sizeof(float)) * gn_head_floats(G, threads / (C / 8)); }
 
 // CTAs to a cluster of the one-kernel form, 0 where a sample does not fit.
 static int gn_cluster(int64_t samples, int64_t rows, int32_t C, int32_t G) {
-  const size_t room = kGnSmem - gn_head_bytes(C, G) - gn_part_bytes(C);
+  const size_t room = kGnSmem - gn_head_bytes(C, G, gn_threads(C)) - gn_part_bytes(C);
   int cs = 1;
   while (cs <= kGnMaxCluster && static_cast<size_t>((rows + cs - 1) / cs) * C * 2 > room) cs *= 2;
   if (cs > kGnMaxCluster) return 0;
   while (cs < kGnMaxCluster && samples * cs * 2 <= 148 && rows >= 4 * cs) cs *= 2;
   return cs;
 }
-static int gn_chunks(int64_t samples, int64_t rows) {
-  // about one CTA of 20 warps to an SM, 16 rows or more to each
-  int64_t c = 148 / samples;
-  c = c < 1 ? 1 : c > kGnMaxChunks ? kGnMaxChunks : c;
-  const int64_t most = (rows + 15) / 16;
-  return static_cast<int>(c < most ? c : most < 1 ? 1 : most);
+// CTAs to a sample of the two-kernel form, where `ctas` fill the device: 16 rows or more to each
+static int gn_chunks(int64_t samples, int64_t rows, int ctas) {
+  const int64_t c = ctas / samples, most = (rows + 15) / 16;
+  return static_cast<int>(c < 1 ? 1 : c < most ? c : most);
 }
 size_t group_norm_workspace(int64_t samples, int64_t rows, int32_t C, int32_t G) {
   if (samples <= 0 || rows <= 0 || C < 8 || gn_cluster(samples, rows, C, G) != 0) return 256;
-  return (static_cast<size_t>(samples) * gn_chunks(samples, rows) * G * sizeof(float2) + 255) & ~static_cast<size_t>(255);
+  return (static_cast<size_t>(samples) * gn_chunks(samples, rows, 148) * G * sizeof(float2) + 255) & ~static_cast<size_t>(255);
 }
 
 #define GN_PICK(KERNEL, codes, silu) \
@@ -526,10 +526,10 @@ int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, i
                       void* workspace, cudaStream_t stream) {
   GnArgs a{static_cast<const uint16_t*>(x), rows, ldx, C, G, C / G, ((1ull << 32) + C / G - 1) / (C / G), static_cast<const uint16_t*>(gamma),
            static_cast<const uint16_t*>(beta), eps, 1.0 / (static_cast<double>(rows) * (C / G)), static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
-           static_cast<float2*>(workspace), 0, 0};
+           static_cast<float2*>(workspace), 0, 0, 0, 0};
   const bool codes = q != nullptr;
   const int threads = gn_threads(C);
-  const size_t head = gn_head_bytes(C, G), part = gn_part_bytes(C);
+  const size_t head = gn_head_bytes(C, G, threads), part = gn_part_bytes(C);
   cudaError_t e = cudaSuccess;
   if (const int cs = gn_cluster(samples, rows, C, G); cs != 0) {
     a.chunks = cs;
@@ -537,11 +537,19 @@ int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, i
     e = launch_cluster(GN_PICK(gn_cluster_kernel, codes, silu), dim3(static_cast<unsigned>(samples * cs)), dim3(threads),
                        head + part + static_cast<size_t>(a.chunk_rows) * C * 2, stream, true, static_cast<unsigned>(cs), a);
   } else {
-    a.chunks = gn_chunks(samples, rows);
+    a.chunks = gn_chunks(samples, rows, 148);
     a.chunk_rows = (rows + a.chunks - 1) / a.chunks;
-    const dim3 grid(static_cast<unsigned>(samples * a.chunks));
-    e = launch(gn_stats_kernel, grid, dim3(threads), part, stream, true, a);
-    if (e == cudaSuccess) e = launch(GN_PICK(gn_apply_kernel, codes, silu), grid, dim3(threads), head, stream, true, a);
+    // Codes wait for their rows' maxima: two CTAs of ten warps to an SM, one of which works while the other waits (8 x 4096 x 320 with
+    // SiLU 19.0 -> 18.0 us, 128 x 1400 x 320 87.6 -> 83.3; four of five warps 17.7 / 81.8, but 2 x 1023 x 640 10.2 -> 12.6). Rows of
+    // more than 1280 channels leave such a CTA one at a time (8 x 256 x 1920 13.0 -> 17.2): one of twenty warps.
+    const bool halves = codes && C <= 1280;
+    const int out_threads = halves ? gn_threads(C, kGnMaxThreads / 2) : threads;
+    a.out_chunks = halves ? gn_chunks(samples, rows, 296) : a.chunks;
+    a.out_rows = (rows + a.out_chunks - 1) / a.out_chunks;
+    e = launch(gn_stats_kernel, dim3(static_cast<unsigned>(samples * a.chunks)), dim3(threads), part, stream, true, a);
+    if (e == cudaSuccess)
+      e = launch(GN_PICK(gn_apply_kernel, codes, silu), dim3(static_cast<unsigned>(samples * a.out_chunks)), dim3(out_threads),
+                 gn_head_bytes(C, G, out_threads), stream, true, a);
   }
   if (e != cudaSuccess) return fail(DP_ERR_CUDA, "group norm launch failed: %s", cudaGetErrorString(e));
   return DP_OK;

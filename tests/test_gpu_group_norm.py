@@ -69,6 +69,12 @@ def test_codes(n, rows, C, G, act):
     _check_codes(q, s_a, x, C, n, rows, G, gamma, beta, act)
 
 
+@pytest.mark.parametrize("n,rows,C,G", [(3, 1301, 320, 32), (200, 600, 192, 8), (1, 5000, 1280, 32), (3, 700, 1296, 9), (2, 601, 1920, 32)])
+def test_codes_of_maps_beyond_shared_memory(n, rows, C, G):
+    """The second kernel's CTAs are cut unlike the first's up to 1280 channels, and like them beyond."""
+    test_codes(n, rows, C, G, B.DP_ACT_SILU)
+
+
 @pytest.mark.parametrize("n,rows,C,G", [(2, 70, 320, 32), (1, 2000, 64, 4), (2, 9, 2560, 32)])
 def test_pitches(n, rows, C, G):
     x, gamma, beta = _inputs(n, rows, C, 3, ldx=C + 40)
