@@ -655,11 +655,11 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   p.scale_by_cap = a->cap != 0.0f ? static_cast<float>(fmin(2.0 * log2e * a->scale / a->cap, 3.0e38)) : 0.0f;
   p.causal = a->mask == DP_MASK_CAUSAL;
   p.status = device_status;
-  // A tile of 128 queries on tcgen05 beats 16-row fragments as soon as there is more than a handful of either: 8 x 40 queries over
-  // 1000 keys, 16 heads of 72: 17.5 against 36 us; 64 x 96 over 96: 20 / 37; but 128 x 64 over 64: 43 / 27, one query over 4096
-  // keys (8 sequences): 48 / 33.
+  // Few queries over long contexts go to the kernel that cuts the keys over CTAs (its rule says how few), else a tile of 128 queries on
+  // tcgen05 beats 16-row fragments as soon as there is more than a handful of either: 8 x 40 queries over 1000 keys, 16 heads of 72: 17.5
+  // against 36 us; 64 x 96 over 96: 20 / 37; but 128 x 64 over 64: 43 / 27.
   const int64_t rows = a->max_q * (H / KV);
-  const bool few = rows <= 32 || (rows <= 64 && a->max_k <= 64);
+  const bool few = rows <= 32 || (rows <= 64 && a->max_k <= 64) || attn_cuts_keys(p);
   if (Mk == 0 || (flags & DP_FLAG_FORCE_SIMT) || (few && !(flags & DP_FLAG_FORCE_MMA)))
     return launch_attn_rows(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));
   return launch_attn_tc(p, static_cast<cudaStream_t>(stream), !(flags & DP_FLAG_NO_PDL));

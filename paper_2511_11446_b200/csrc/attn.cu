@@ -136,17 +136,21 @@ __device__ __forceinline__ uint16_t* at_out(const AttnParams& p, const AttnSeq& 
   return p.y + static_cast<int64_t>(s.q0 + at.tok(row)) * p.ldy + at.head(row) * p.y_hs;
 }
 
-// 16 MB rows by every one of W warps, each with keys of its own. grid.x = splits * KV * n_seq, clusters of `splits` along x.
+// 16 MB rows by every one of W warps, each with keys of its own. grid.x = splits * row_blocks * KV * n_seq, clusters of `splits` along x;
+// row_blocks: blocks of 16 MB rows of the longest sequence.
 template <int DP, int MB, int W>
 __global__ void __launch_bounds__(32 * W)
-attn_few_kernel(const AttnParams p, const int splits) {
+attn_few_kernel(const AttnParams p, const int splits, const int row_blocks) {
   constexpr int ROWS = 16 * MB, RB = at_row_bytes(DP), KS = DP / 16, NB = DP / 8, OW = DP + 4;
   constexpr int STAGE = 2 * few_keys(DP, MB) * RB;
   constexpr int kFewKeys = few_keys(DP, MB), kFewStages = few_stages(DP, MB);
   extern __shared__ __align__(128) uint8_t at_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
-  const int split = blockIdx.x % splits, u = blockIdx.x / splits;
+  const int split = blockIdx.x % splits;
+  int u = blockIdx.x / splits;
+  const int block = u % row_blocks;
+  u /= row_blocks;
   const int kvh = u % p.KV, group = p.H / p.KV;
   uint8_t* ring = at_smem + warp * kFewStages * STAGE;
   if (p.D < DP)  // the columns of padding between D and DP are zero throughout
@@ -156,10 +160,12 @@ attn_few_kernel(const AttnParams p, const int splits) {
     }
   pdl_wait();
   const AttnSeq s = attn_seq(p, u / p.KV);
-  const int rows = s.nq * group;  // (at most 16 MB)
-  if (rows == 0) return;  // (the whole cluster)
-  const AtPlace at{0, 0, rows, group, kvh};
-  const int keys = attn_keys(p, s, s.nq - 1);
+  const int tok0 = block * ROWS / group;
+  const int64_t all = static_cast<int64_t>(s.nq) * group - block * ROWS;
+  if (all <= 0) return;  // (the whole cluster)
+  const int rows = static_cast<int>(min(all, static_cast<int64_t>(ROWS)));
+  const AtPlace at{tok0, block * ROWS - tok0 * group, rows, group, kvh};
+  const int keys = attn_keys(p, s, at.tok(rows - 1));
   const int n = (keys + kFewKeys - 1) / kFewKeys, parts = splits * W, part_at = split * W + warp;
   const int begin = static_cast<int>(static_cast<int64_t>(n) * part_at / parts), end = static_cast<int>(static_cast<int64_t>(n) * (part_at + 1) / parts);
   const uint16_t* kp = p.k + static_cast<int64_t>(s.k0) * p.ldk + kvh * p.k_hs;
@@ -481,10 +487,29 @@ constexpr size_t at_few_smem() {
   constexpr size_t join = (W + 1) * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
   return ring > join ? ring : join;
 }
+// Clusters of 1 .. 8 CTAs that a device holds at once (a cluster stays within a group of 16 to 18 SMs), found when it is first used;
+// devices of one architecture have the same.
+template <int DP, int MB, int W>
+static int g_few_fit[kAtMaxSplits + 1];
 template <int DP, int MB, int W>
 static cudaError_t at_few_init() {
-  return cudaFuncSetAttribute(attn_few_kernel<DP, MB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(at_few_smem<DP, MB, W>()));
+  cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<DP, MB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(at_few_smem<DP, MB, W>()));
+  for (int splits = 1; splits <= kAtMaxSplits && e == cudaSuccess; ++splits) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(splits * 1024));
+    cfg.blockDim = dim3(32 * W);
+    cfg.dynamicSmemBytes = at_few_smem<DP, MB, W>();
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(splits);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&g_few_fit<DP, MB, W>[splits], attn_few_kernel<DP, MB, W>, &cfg);
+  }
+  return e;
 }
 template <int DP>
 static int at_init() {
@@ -505,44 +530,56 @@ int attn_init_device() {
 }
 
 template <int DP, int MB, int W>
-static cudaError_t launch_few(const AttnParams& p, unsigned grid, int splits, cudaStream_t stream, bool pdl) {
-  return launch_cluster(attn_few_kernel<DP, MB, W>, dim3(grid), dim3(32 * W), at_few_smem<DP, MB, W>(), stream, pdl,
-                        static_cast<unsigned>(splits), p, splits);
+static cudaError_t launch_few(const AttnParams& p, int64_t units, int row_blocks, cudaStream_t stream, bool pdl) {
+  // Each unit's keys over as many CTAs, up to eight, as all run at once, and as long as a warp has a tile of keys. (Six CTAs to each of 48
+  // units, for which there are SMs but no places: 3 sequences of 16 x 72, 8192 keys 39.6 us, 26.1 by five; and with three
+  // to each of 80, which fit, 39.1 us, by two 51.2.)
+  const int64_t tiles_of_keys = (static_cast<int64_t>(p.max_k) + 31) / 32;
+  int splits = static_cast<int>(tiles_of_keys / W < kAtMaxSplits ? tiles_of_keys / W : kAtMaxSplits);
+  while (splits > 1 && g_few_fit<DP, MB, W>[splits] < units) --splits;
+  splits = splits < 1 ? 1 : splits;
+  return launch_cluster(attn_few_kernel<DP, MB, W>, dim3(static_cast<unsigned>(units * splits)), dim3(32 * W), at_few_smem<DP, MB, W>(),
+                        stream, pdl, static_cast<unsigned>(splits), p, splits, row_blocks);
 }
+// tiles: of attn_rows_kernel; 0: attn_few_kernel.
 template <int DP>
-static cudaError_t launch_at(const AttnParams& p, unsigned grid, int tiles, int splits, int warps, int64_t rows, cudaStream_t stream,
-                             bool pdl) {
-  if (tiles > 0) return launch(attn_rows_kernel<DP>, dim3(grid), dim3(kAtThreads), at_rows_smem<DP>(), stream, pdl, p, tiles);
-  return warps == 4 ? rows <= 16 ? launch_few<DP, 1, 4>(p, grid, splits, stream, pdl) : launch_few<DP, 2, 4>(p, grid, splits, stream, pdl)
-                    : rows <= 16 ? launch_few<DP, 1, 8>(p, grid, splits, stream, pdl) : launch_few<DP, 2, 8>(p, grid, splits, stream, pdl);
+static cudaError_t launch_at(const AttnParams& p, int64_t units, int64_t tiles, int64_t rows, cudaStream_t stream, bool pdl) {
+  if (tiles > 0)
+    return launch(attn_rows_kernel<DP>, dim3(static_cast<unsigned>(units)), dim3(kAtThreads), at_rows_smem<DP>(), stream, pdl, p,
+                  static_cast<int>(tiles));
+  // CTAs of eight warps where there are only a few units (4 of 128, 8192 keys: 18.5 us by four warps, 15.4 by eight; 16 of 72: 17.5
+  // and 22, since clusters of eight whole SMs are hard to place).
+  const bool wide = units <= 8;
+  if (rows <= 16) return wide ? launch_few<DP, 1, 8>(p, units, 1, stream, pdl) : launch_few<DP, 1, 4>(p, units, 1, stream, pdl);
+  const int blocks = static_cast<int>((rows + 31) / 32);
+  return wide ? launch_few<DP, 2, 8>(p, units, blocks, stream, pdl) : launch_few<DP, 2, 4>(p, units, blocks, stream, pdl);
+}
+
+static int64_t few_units(const AttnParams& p) {  // blocks of 32 rows of a key head
+  return (static_cast<int64_t>(p.max_q) * (p.H / p.KV) + 31) / 32 * p.KV * p.n_seq;
+}
+// Whether the keys are cut over clusters, for blocks of 32 rows: always where there is one, and of more where that makes few units of long
+// contexts, which would leave the tcgen05 kernel's tiles of 128 on few SMs. (Up to 64 units and from 769 keys on; 16 heads of 72, one
+// sequence: 128 queries = 64 units, 1024 / 4096 / 8192 keys 14 / 27 / 43 us against 17 / 50 / 95 on tcgen05; 16 heads of 128 on 4 key heads: 18 / 40 /
+// 66 against 18 / 55 / 102. 512 keys 11 and 14 against 12; 128 units 19 / 43 / 74 against 17 / 50 / 95, and 27 / 67 / 118 against 18 / 55 / 103.)
+// With a tile of keys or less there is nothing to cut: the kernel whose warps share it (256 sequences of 32, 16 heads of 72: 48 us
+// against 87).
+bool attn_cuts_keys(const AttnParams& p) {
+  const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
+  return p.max_k > kAtKeys && (rows <= 32 || (p.max_k > 768 && few_units(p) <= 64));
 }
 
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
-  // With a tile of keys or less there is nothing to split: the kernel whose warps share it (256 sequences of 32, 16 heads of 72:
-  // 48 us against 87).
-  const bool few = rows <= 32 && p.max_k > kAtKeys;
-  const int64_t tiles = few ? 0 : (rows + 63) / 64;
-  const int64_t units = (few ? 1 : tiles) * p.KV * p.n_seq;
-  int splits = 1, warps = 4;
-  if (few) {
-    // As many CTAs of four warps as the SMs hold, two each, up to eight to a (sequence, head) pair, as long as a warp has a tile of
-    // keys; of eight warps where there are only a few pairs. (4 pairs of 4 x 128, 8192 keys: 18.5 us by four warps, 15.4 by eight;
-    // 16 pairs of 72: 17.5 and 22, since clusters of eight whole SMs are hard to place.)
-    warps = units <= 8 ? 8 : 4;
-    const int64_t most = (warps == 8 ? 1 : 2) * num_sms() / units, tiles_of_keys = (static_cast<int64_t>(p.max_k) + 31) / 32;
-    splits = static_cast<int>(tiles_of_keys / warps < most ? tiles_of_keys / warps : most);
-    splits = splits < 1 ? 1 : splits > kAtMaxSplits ? kAtMaxSplits : splits;
-  }
-  if (units * splits > 0x7FFFFFFF || tiles > 0x7FFFFFFF)
+  const bool few = attn_cuts_keys(p);
+  const int64_t tiles = few ? 0 : (rows + 63) / 64, units = few ? few_units(p) : tiles * p.KV * p.n_seq;
+  if (units > 0x7FFFFFFF / kAtMaxSplits || tiles > 0x7FFFFFFF)
     return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)units);
-  const unsigned grid = static_cast<unsigned>(units * splits);
-  const int t = static_cast<int>(tiles);
-  const cudaError_t e = p.D <= 32   ? launch_at<32>(p, grid, t, splits, warps, rows, stream, pdl)
-                        : p.D <= 64 ? launch_at<64>(p, grid, t, splits, warps, rows, stream, pdl)
-                        : p.D <= 80 ? launch_at<80>(p, grid, t, splits, warps, rows, stream, pdl)
-                        : p.D <= 96 ? launch_at<96>(p, grid, t, splits, warps, rows, stream, pdl)
-                                    : launch_at<128>(p, grid, t, splits, warps, rows, stream, pdl);
+  const cudaError_t e = p.D <= 32   ? launch_at<32>(p, units, tiles, rows, stream, pdl)
+                        : p.D <= 64 ? launch_at<64>(p, units, tiles, rows, stream, pdl)
+                        : p.D <= 80 ? launch_at<80>(p, units, tiles, rows, stream, pdl)
+                        : p.D <= 96 ? launch_at<96>(p, units, tiles, rows, stream, pdl)
+                                    : launch_at<128>(p, units, tiles, rows, stream, pdl);
   if (e != cudaSuccess) return fail(DP_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
   return DP_OK;
 }

@@ -55,6 +55,7 @@ int group_norm_init_device();
 // attn.cu -- attention, mma.sync tiles of 16 queries
 struct AttnParams;
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl);
+bool attn_cuts_keys(const AttnParams& p);  // whether it cuts the keys over clusters of CTAs, for few queries
 int attn_init_device();
 // attn_tc.cu -- attention, tcgen05 tiles of 128 queries
 int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl);

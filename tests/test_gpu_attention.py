@@ -141,6 +141,18 @@ def test_few_queries_over_long_contexts(H, KV, D, flags):
 
 
 @pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("H,KV,D", [(6, 2, 72), (16, 1, 128), (4, 4, 64), (5, 1, 40), (7, 1, 96), (40, 1, 8)])
+def test_blocks_of_rows_over_long_contexts(H, KV, D, causal, flags):
+    """More (query, head) rows than a block of 32, a query's heads in two blocks, keys cut over CTAs; sequences that end within
+    a block, one without queries."""
+    lq, lk = [20, 3, 0, 1, 17], [1500, 900, 640, 1, 33]
+    _run(H, KV, D, lq, lk, causal=causal, layout="rows", pad=3, flags=flags, seed=H)
+    _run(H, KV, D, lq, lk, causal=True, prefix=[0, 700, 5, 1, 40], cap=20.0, layout="heads", flags=flags, seed=D,
+         slopes=torch.linspace(0.5, 0.004, H, device="cuda"))
+
+
+@pytest.mark.parametrize("flags", FORMS)
 def test_scores_of_large_spread(flags):
     """One key takes all the weight, and the running maximum jumps from tile to tile."""
     _run(2, 2, 64, [300], [300], flags=flags, spread=40.0)
