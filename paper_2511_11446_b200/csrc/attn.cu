@@ -559,14 +559,14 @@ static int64_t few_units(const AttnParams& p) {  // blocks of 32 rows of a key h
   return (static_cast<int64_t>(p.max_q) * (p.H / p.KV) + 31) / 32 * p.KV * p.n_seq;
 }
 // Whether the keys are cut over clusters, for blocks of 32 rows: always where there is one, and of more where that makes few units of long
-// contexts, which would leave the tcgen05 kernel's tiles of 128 on few SMs. (Up to 64 units and from 769 keys on; 16 heads of 72, one
-// sequence: 128 queries = 64 units, 1024 / 4096 / 8192 keys 14 / 27 / 43 us against 17 / 50 / 95 on tcgen05; 16 heads of 128 on 4 key heads: 18 / 40 /
-// 66 against 18 / 55 / 102. 512 keys 11 and 14 against 12; 128 units 19 / 43 / 74 against 17 / 50 / 95, and 27 / 67 / 118 against 18 / 55 / 103.)
+// contexts, which would leave the tcgen05 kernel's tiles of 128 on few SMs. (From 769 keys on and up to 64 units, 40 of more than 96 columns. 16 heads of
+// 72, one sequence: 128 queries = 64 units, 1024 / 4096 keys 14 / 27 us against 15 / 40 on tcgen05, 256 queries 19 / 43 against 15 / 40; 512 keys 11 and 12; heads
+// of 128, 100 queries: 32 units 14 / 27 against 15 / 38, 64 units 18 / 40 against 15 / 38.)
 // With a tile of keys or less there is nothing to cut: the kernel whose warps share it (256 sequences of 32, 16 heads of 72: 48 us
 // against 87).
 bool attn_cuts_keys(const AttnParams& p) {
   const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
-  return p.max_k > kAtKeys && (rows <= 32 || (p.max_k > 768 && few_units(p) <= 64));
+  return p.max_k > kAtKeys && (rows <= 32 || (p.max_k > 768 && few_units(p) <= (p.D <= 96 ? 64 : 40)));
 }
 
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {

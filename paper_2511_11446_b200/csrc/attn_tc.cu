@@ -11,6 +11,7 @@
 // Tensor memory, 512 columns: S0 S1, P0 P1 (half as wide), O0 O1. P stands beside S, so that the next scores are computed while a
 // warpgroup still takes exponentials; that asks for 2 (3/2 BN + D) columns: 128 keys to a tile up to D = 64, 96 up to D = 96, 80 up
 // to 128 (P over S with 128 keys there, measured: 8192 tokens causal with distance bias, 16 heads of 128: 342 us).
+// Where an item of 128 queries is all there is (CUT), the warpgroups take its key tiles in turn and the first joins their sums.
 // A warp beside them decodes the work items ahead of everybody (a dozen divisions and the sequences' offsets), through a small
 // ring in shared memory.
 //
@@ -47,13 +48,14 @@ struct TcForm {
   static constexpr int NS = NBLK == 1 ? 8 : BN == 96 ? 6 : 7;  // ring stages
   static constexpr uint32_t kS = 0, kP = 2 * BN, kO = 3 * BN;  // columns
   static_assert(BN % 16 == 0 && kO + 2 * D <= 512, "tensor memory");
-  // (after the tiles: the ring of items, the sequences' order, barriers, turns, tensor memory's address, the abort flag)
-  static constexpr size_t kSmem = 1024 + 2 * kQBytes + NS * kKvBytes + 4 * 48 + kTcOrderBytes + (2 * NS + 12 + 2 * 4) * 8 + 48;
+  // (after the tiles: rows' maxima and sums, the ring of items, the sequences' order, barriers, turns, tensor memory's address, the abort flag)
+  static constexpr size_t kSmem = 1024 + 2 * kQBytes + NS * kKvBytes + 1024 + 4 * 48 + kTcOrderBytes + (2 * NS + 14 + 2 * 4) * 8 + 48;
   static_assert(kSmem <= 232448, "shared memory");
 };
 
 struct AttnTcSched {
   int32_t rows;        // queries of a work item: 128 or 256
+  int32_t cut;         // whether its two warpgroups share the keys of 128 queries
   int32_t tiles;       // items of the longest sequence
   int32_t items;       // tiles * heads * sequences
   int32_t group;       // (sequence, head) pairs whose items are taken together, longest ones first
@@ -246,9 +248,9 @@ __device__ __forceinline__ void tc_store_32(uint16_t* y, int64_t ld, int row0, i
 struct __align__(16) TcItem {
   AttnSeq s;
   int head, row0;    // row0 < 0: no more items
-  int n0, n1;        // key tiles of the two tiles of queries
+  int n0, n1;        // key tiles of the two tiles of queries, or (cut) of the two warpgroups
   int live0, live1;  // queries in them
-  __device__ __forceinline__ int n() const { return max(n0, n1); }
+  __device__ __forceinline__ int n(bool cut) const { return cut ? n0 + n1 : max(n0, n1); }
 };
 constexpr int kTcSorted = 64;
 constexpr int kTcSlots = 4;      // of the ring of items
@@ -262,6 +264,11 @@ __device__ __forceinline__ bool tc_item(const AttnParams& p, const AttnTcSched& 
   r.live0 = min(r.s.nq - r.row0, kTcTile);
   r.live1 = c.rows > kTcTile ? min(max(r.s.nq - r.row0 - kTcTile, 0), kTcTile) : 0;
   r.n0 = (attn_keys(p, r.s, r.row0 + r.live0 - 1) + BN - 1) / BN;
+  if (c.cut) {
+    r.n1 = r.n0 / 2;
+    r.n0 -= r.n1;
+    return true;
+  }
   r.n1 = r.live1 > 0 ? (attn_keys(p, r.s, r.row0 + kTcTile + r.live1 - 1) + BN - 1) / BN : 0;
   return true;
 }
@@ -362,7 +369,8 @@ __device__ __forceinline__ bool tc_next(const AttnParams& p, const AttnTcSched& 
   }
 }
 
-template <int KS, bool CAP, bool BIAS>
+// CUT: items of one tile of queries, whose key tiles the warpgroups take in turn (even ones, odd ones); their sums are joined at the end.
+template <int KS, bool CAP, bool BIAS, bool CUT>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                const __grid_constant__ CUtensorMap tv, const AttnParams p, const AttnTcSched c) {
@@ -372,7 +380,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                    // [2][NBLK][128 rows][128 bytes]
   uint8_t* sKV = sQ + 2 * F::kQBytes;    // [NS][NBLK][BN rows][128 bytes]
-  TcItem* slots = reinterpret_cast<TcItem*>(sKV + NS * F::kKvBytes);
+  float2* half = reinterpret_cast<float2*>(sKV + NS * F::kKvBytes);  // [128]
+  TcItem* slots = reinterpret_cast<TcItem*>(half + kTcTile);
   TcOrder* order = reinterpret_cast<TcOrder*>(slots + kTcSlots);
   uint64_t* full = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(order) + kTcOrderBytes);
   uint64_t* empty = full + NS;
@@ -384,7 +393,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
   uint64_t* s_read = s_full + 2;   // [2] and in the warpgroup's registers
   uint64_t* p_full = s_read + 2;   // [2] weights are there
   uint64_t* pv_done = p_full + 2;  // [2] and their product has ended
-  volatile uint32_t* turns = reinterpret_cast<uint32_t*>(pv_done + 2);  // [8] tiles whose exponentials a warp has taken
+  uint64_t* half_full = pv_done + 2;     // the second warpgroup's half of the keys is summed
+  uint64_t* half_read = half_full + 1;   // and in the first one's registers
+  volatile uint32_t* turns = reinterpret_cast<uint32_t*>(half_read + 1);  // [8] tiles whose exponentials a warp has taken
   uint32_t* tmem_slot = const_cast<uint32_t*>(turns) + 8;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -407,6 +418,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       mbar_init(&p_full[t], 4);
       mbar_init(&pv_done[t], 1);
     }
+    mbar_init(half_full, 4);
+    mbar_init(half_read, 4);
     *abort_flag = 0;
     fence_barrier_init();
     tma_prefetch_desc(&tq);
@@ -455,10 +468,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         mbar_arrive_expect_tx(&q_full[t], F::kQBytes);
 #pragma unroll
         for (int b = 0; b < NBLK; ++b)
-          tma_load_3d(smem_u32(sQ) + t * F::kQBytes + b * kTcBlock, &tq, b * 64, it.head, it.s.q0 + it.row0 + t * kTcTile, &q_full[t]);
+          tma_load_3d(smem_u32(sQ) + t * F::kQBytes + b * kTcBlock, &tq, b * 64, it.head, it.s.q0 + it.row0 + (CUT ? 0 : t * kTcTile), &q_full[t]);
       };
       while (ok && (ok = next_item(it, false)) && it.row0 >= 0) {
-        const int n = it.n();
+        const int n = it.n(CUT);
         if (it.n0 > 0) load_q(0);
         const int kvh = it.head / group;
         for (int j = 0; j < 2 * n && ok; ++j) {  // K, V, K, V, ..
@@ -522,14 +535,22 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         if (ok && n == 1) mma_commit(&q_empty[t]);
       };
       Ring st;  // K of the item's first tile
+      auto pass_on = [&](int stages) {  // the other tile's
+        for (int j = 0; j < stages && ok; ++j) {
+          if (!(ok = tc_wait(&full[st.s], st.ph, abort_flag, c.budget))) break;
+          mbar_arrive(&empty[st.s]);
+          st.next(NS);
+        }
+      };
       TcItem nxt;
       ok = next_item(nxt, false);
       while (ok && nxt.row0 >= 0) {
-        const int n_all = nxt.n(), n = t ? nxt.n1 : nxt.n0;
+        const int n_all = nxt.n(CUT), n = t ? nxt.n1 : nxt.n0;
         if (!(ok = next_item(nxt, false))) break;
         const int n_next = nxt.row0 >= 0 ? (t ? nxt.n1 : nxt.n0) : 0;
         if (n > 0) {
-          if (!ahead) first_scores(st, n);
+          if (CUT && t == 1) pass_on(2);
+          if (!ahead && ok) first_scores(st, n);
           ahead = false;
           st.next(NS);
           for (int j = 0; j < n && ok; ++j) {
@@ -539,7 +560,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
               scores(st);
               if (ok && j + 2 == n) mma_commit(&q_empty[t]);
             };
-            if (j + 1 < n) next_scores();
+            if (CUT && j + 1 < n) pass_on(2);
+            if (ok && j + 1 < n) next_scores();
             if (!ok || !(ok = tc_wait(&p_full[t], n_p & 1, abort_flag, c.budget)) || !(ok = tc_wait(&full[v.s], v.ph, abort_flag, c.budget))) break;
             ++n_p;
             tc_fence_after();
@@ -552,18 +574,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
             mma_commit(&empty[v.s]);
             if (j + 1 < n) {
               st.next(NS);
-            } else if (n == n_all && n_next > 0) {  // the next item's first scores while this one's output is written
+            } else if (!CUT && n == n_all && n_next > 0) {  // the next item's first scores while this one's output is written
               first_scores(st, n_next);
               ahead = true;
             }
           }
         }
         // the rest of the item's tiles is the other tile's: passed on as they come
-        for (int j = 2 * n; j < 2 * n_all && ok; ++j) {
-          if (!(ok = tc_wait(&full[st.s], st.ph, abort_flag, c.budget))) break;
-          mbar_arrive(&empty[st.s]);
-          st.next(NS);
-        }
+        pass_on(2 * (n_all - (CUT && n > 0 ? 2 * n - 1 + t : n)));
       }
     }
   } else {
@@ -575,11 +593,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
     const uint32_t a_s = lanes + F::kS + t * BN, a_p = lanes + F::kP + t * (BN / 2), a_o = lanes + F::kO + t * F::D;
     Ring st;
     bool ok = true;
-    uint32_t n_s = 0, others = 0;  // tiles so far, the other warpgroup's up to this item
+    uint32_t n_s = 0, others = 0, joins = 0;  // tiles so far, the other warpgroup's up to this item, items joined
     TcItem it;
     while (ok && (ok = next_item(it, true)) && it.row0 >= 0) {
-      const int n_all = it.n(), n = t ? it.n1 : it.n0, live = t ? it.live1 : it.live0;
-      const int pos = it.row0 + t * kTcTile + row + it.s.behind;  // of this thread's query
+      const int n_all = it.n(CUT), n = t ? it.n1 : it.n0, live = t ? it.live1 : it.live0;
+      const int pos = it.row0 + (CUT ? 0 : t * kTcTile) + row + it.s.behind;  // of this thread's query
       // keys below this bound are visible
       const int bound = p.causal ? min(it.s.nk, max(pos + 1, it.s.prefix)) : it.s.nk;
       const float slope = BIAS ? ld_global_f32(p.slopes + it.head) * kLog2e : 0.0f;
@@ -589,7 +607,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         st.next(NS);  // (K)
         const Ring v = st;
         st.next(NS);
-        if (j >= n) continue;
+        if (CUT ? (j & 1) != t : j >= n) continue;
+        const int own = CUT ? j >> 1 : j;
         ok = tc_wait(&s_full[t], n_s & 1, abort_flag, c.budget);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
@@ -629,7 +648,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
           tc_fence_after();
           return ok;
         };
-        if (j == 0) {
+        if (own == 0) {
           m = top;
         } else if (__any_sync(0xFFFFFFFFu, top > m + kTcRise)) {
           if (!product_before()) break;
@@ -650,13 +669,19 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         // The two warps of an SM quarter take turns at the exponentials: both at once would be no faster, and apart one's stand
         // beside the other's loads, scans and waits (32 x 1024 tokens, 16 heads of 72: 250 us without turns, 237 with). A
         // bounded wait: what it orders is time, not data.
-        const uint32_t until = others + min(j + t, t ? it.n0 : it.n1);
+        const uint32_t until = others + min(own + t, t ? it.n0 : it.n1);
         for (int i = 0; i < 64 && turns[warp ^ 4] < until; ++i) {
         }
         uint32_t w[BN / 2];
         l += tc_weights(s, scale, sub, w);
         if (!(l < 0.0f)) turns[warp] = n_s + 1;  // (never negative: the store waits for the sum)
         if (!product_before()) break;
+        if (CUT && t == 1 && own == 0 && joins > 0) {  // (the last item's sums are read: this product overwrites them)
+          ok = tc_wait(half_read, (joins - 1) & 1, abort_flag, c.budget);
+          ok = __all_sync(0xFFFFFFFFu, ok);
+          if (!ok) break;
+          tc_fence_after();
+        }
         ++n_s;
 #pragma unroll
         for (int k = 0; k < BN / 32; ++k) tmem_st_x16(a_p + k * 16, w + k * 16);
@@ -680,7 +705,32 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       }
       if (!ok) break;
       others += t ? it.n0 : it.n1;
+      if (CUT && t == 1 && n > 0) {
+        ok = tc_wait(&pv_done[1], (n_s - 1) & 1, abort_flag, c.budget);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        half[row] = make_float2(m, l);
+        ++joins;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(half_full);
+      }
       if (live == 0) continue;
+      float mine = 1.0f, other = 0.0f;  // shares of the two halves of the keys
+      const bool join = CUT && it.n1 > 0;
+      if (join) {
+        ok = tc_wait(half_full, joins & 1, abort_flag, c.budget);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        ++joins;
+        tc_fence_after();
+        const float2 h = half[row];
+        const float top = fmaxf(m, h.x), sub = top == -INFINITY ? 0.0f : top;
+        mine = ex2(m - sub);
+        other = ex2(h.x - sub);
+        l = fmaf(l, mine, h.y * other);
+      }
       const float inv = l != 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;  // (no key in sight: O is zero too)
       uint16_t* yt = p.y + static_cast<int64_t>(it.s.q0 + it.row0 + t * kTcTile) * p.ldy + it.head * p.y_hs;
       float o[(F::D + 31) / 32 * 32];
@@ -692,6 +742,19 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
 #pragma unroll
         for (int k = 0; k < F::D; k += 16) tmem_ld_x16(a_o + k, o + k);
         tmem_ld_wait();
+        if (join) {
+#pragma unroll
+          for (int k = 0; k < F::D; k += 16) {
+            float h[16];
+            tmem_ld_x16(lanes + F::kO + F::D + k, h);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[k + i] = fmaf(o[k + i], mine, h[i] * other);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(half_read);
+        }
         tc_fence_before();  // (the next item's products write O behind this thread's next arrival on p_full)
       } else {
 #pragma unroll
@@ -722,8 +785,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
 // ---- host side -------------------------------------------------------------------------------------
 template <int KS, bool CAP, bool BIAS>
 static cudaError_t tc_init() {
-  return cudaFuncSetAttribute(attn_tc_kernel<KS, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(TcForm<KS>::kSmem));
+  cudaError_t e = cudaFuncSetAttribute(attn_tc_kernel<KS, CAP, BIAS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(TcForm<KS>::kSmem));
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(attn_tc_kernel<KS, CAP, BIAS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 static_cast<int>(TcForm<KS>::kSmem));
 }
 template <int KS>
 static int tc_init_ks() {
@@ -741,7 +807,7 @@ int attn_tc_init_device() {
   return st;
 }
 
-template <int KS>
+template <int KS, bool CUT>
 static int launch_tc(const AttnParams& p, const AttnTcSched& c, unsigned ctas, cudaStream_t stream, bool pdl) {
   using F = TcForm<KS>;
   CUtensorMap tq, tk, tv;
@@ -752,22 +818,33 @@ static int launch_tc(const AttnParams& p, const AttnTcSched& c, unsigned ctas, c
   const dim3 grid(ctas), block(kTcThreads);
   const bool cap = p.cap != 0.0f, bias = p.slopes != nullptr;
   const cudaError_t e =
-      cap && bias ? launch(attn_tc_kernel<KS, true, true>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
-      : cap       ? launch(attn_tc_kernel<KS, true, false>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
-      : bias      ? launch(attn_tc_kernel<KS, false, true>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
-                  : launch(attn_tc_kernel<KS, false, false>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c);
+      cap && bias ? launch(attn_tc_kernel<KS, true, true, CUT>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+      : cap       ? launch(attn_tc_kernel<KS, true, false, CUT>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+      : bias      ? launch(attn_tc_kernel<KS, false, true, CUT>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c)
+                  : launch(attn_tc_kernel<KS, false, false, CUT>, grid, block, F::kSmem, stream, pdl, tq, tk, tv, p, c);
   if (e != cudaSuccess) return fail(DP_ERR_CUDA, "attention launch failed: %s", cudaGetErrorString(e));
   return DP_OK;
+}
+template <bool CUT>
+static int launch_tc_width(const AttnParams& p, const AttnTcSched& c, unsigned ctas, cudaStream_t stream, bool pdl) {
+  return p.D <= 64   ? launch_tc<4, CUT>(p, c, ctas, stream, pdl)
+         : p.D <= 80 ? launch_tc<5, CUT>(p, c, ctas, stream, pdl)
+         : p.D <= 96 ? launch_tc<6, CUT>(p, c, ctas, stream, pdl)
+                     : launch_tc<8, CUT>(p, c, ctas, stream, pdl);
 }
 
 int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int sms = num_sms() > 0 ? num_sms() : 148;
   const int64_t pairs = static_cast<int64_t>(p.H) * p.n_seq;
   AttnTcSched c;
-  // Items of 256 queries share K and V between two tiles and hide one's products behind the other's exponentials; of 128 where
-  // that many more SMs get work.
+  // Items of 256 queries share K and V between two tiles and hide one's products behind the other's exponentials; of 128, whose
+  // keys the warpgroups share, where that many more SMs get work.
   c.rows = 2 * kTcTile;
   if ((static_cast<int64_t>(p.max_q) + 255) / 256 * pairs * 2 <= sms || p.max_q <= kTcTile) c.rows = kTcTile;
+  // From 385 keys on the second warpgroup, idle otherwise, takes every other tile of the keys of 128 queries (one sequence of 256 queries, 16 heads
+  // of 72, over 256 / 512 / 1000 / 4096 keys: 9.1 / 12.1 / 17.3 / 50.4 us -> 9.2 / 11.6 / 15.3 / 39.9; 64 of 96, over 96 / 200 / 512: 21.1 / 41.4 / 62.7
+  // -> 23.9 / 43.1 / 58.4).
+  c.cut = c.rows == kTcTile && p.max_k > 384;
   const int64_t tiles = (static_cast<int64_t>(p.max_q) + c.rows - 1) / c.rows;
   if (tiles * pairs > 0x7FFFFFFF) return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)(tiles * pairs));
   c.tiles = static_cast<int32_t>(tiles);
@@ -783,10 +860,7 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   // Six items of the most keys there can be, at 8192 cycles a tile (2500 or so are usual), and the items that may not be there,
   // 4096 cycles (800) to 32 of them, on top of the library's usual limit.
   c.budget = kWaitBudgetCycles + 6 * 8192 * (p.Mk / 80 + 1) + 4096 * (c.items / (32ll * ctas) + 1);
-  return p.D <= 64   ? launch_tc<4>(p, c, ctas, stream, pdl)
-         : p.D <= 80 ? launch_tc<5>(p, c, ctas, stream, pdl)
-         : p.D <= 96 ? launch_tc<6>(p, c, ctas, stream, pdl)
-                     : launch_tc<8>(p, c, ctas, stream, pdl);
+  return c.cut ? launch_tc_width<true>(p, c, ctas, stream, pdl) : launch_tc_width<false>(p, c, ctas, stream, pdl);
 }
 
 }  // namespace dp

@@ -152,6 +152,18 @@ def test_blocks_of_rows_over_long_contexts(H, KV, D, causal, flags):
          slopes=torch.linspace(0.5, 0.004, H, device="cuda"))
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D", [64, 72, 96, 128])
+def test_keys_shared_by_two_warpgroups(D, causal):
+    """Items of up to 128 queries of more keys than 384, several to a CTA: odd and even numbers of key tiles, one tile, none; the
+    larger half's scores first or last."""
+    lk = [400, 97, 1, 0, 385, 193, 96, 289, 640, 80] * 5
+    lq = [128, 5, 1, 3, 100, 64, 96, 0, 17, 128] * 5
+    _run(4, 2, D, lq, lk, causal=causal, layout="rows", pad=2, flags=B.DP_FLAG_FORCE_MMA, seed=D)
+    _run(8, 8, D, [100] * 24, [500] * 24, fixed=True, causal=causal, layout="heads", flags=B.DP_FLAG_FORCE_MMA, seed=D + 1, spread=6.0,
+         slopes=torch.linspace(1.0, -0.02, 8, device="cuda"))
+
+
 @pytest.mark.parametrize("flags", FORMS)
 def test_scores_of_large_spread(flags):
     """One key takes all the weight, and the running maximum jumps from tile to tile."""
