@@ -573,7 +573,7 @@ int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
   const bool few = attn_cuts_keys(p);
   const int64_t tiles = few ? 0 : (rows + 63) / 64, units = few ? few_units(p) : tiles * p.KV * p.n_seq;
-  if (units > 0x7FFFFFFF / kAtMaxSplits || tiles > 0x7FFFFFFF)
+  if (units > (few ? 0x7FFFFFFF / kAtMaxSplits : 0x7FFFFFFF) || tiles > 0x7FFFFFFF)
     return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)units);
   const cudaError_t e = p.D <= 32   ? launch_at<32>(p, units, tiles, rows, stream, pdl)
                         : p.D <= 64 ? launch_at<64>(p, units, tiles, rows, stream, pdl)
