@@ -652,7 +652,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
           m = top;
         } else if (__any_sync(0xFFFFFFFFu, top > m + kTcRise)) {
           if (!product_before()) break;
-          const float to_m = fmaxf(m, top), f = to_m == -INFINITY ? 1.0f : ex2(m - to_m);
+          // (only rows whose own maximum has: the warp's others may be queries of another sequence, or nobody's)
+          const float to_m = top > m + kTcRise ? top : m, f = to_m == -INFINITY ? 1.0f : ex2(m - to_m);
           m = to_m;
           l *= f;
 #pragma unroll 1

@@ -1,0 +1,96 @@
+"""What dp_attention's results may depend on: the bits of a sequence's rows are the same whatever finite values stand in other
+sequences' rows, in rows of no sequence and in keys that the mask hides; and rows whose offsets pass 32 bits."""
+import math
+
+import pytest
+import torch
+
+import attention_ref as R
+from paper_2511_11446_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+FORMS = [0, B.DP_FLAG_FORCE_SIMT, B.DP_FLAG_FORCE_MMA]
+
+
+def _starts(lens):
+    return torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
+
+
+def _bits(H, D, lq, lk, q, k, v, causal, cap, slopes, flags):
+    y = torch.zeros(q.shape[0], H * D, dtype=torch.bfloat16, device="cuda")
+    at = B.make_attn(H, H, D, len(lq), max(lq), max(lk), 1 / math.sqrt(D), q_start=_starts(lq), k_start=_starts(lk),
+                     mask=B.DP_MASK_CAUSAL if causal else B.DP_MASK_NONE, cap=cap, slopes=slopes)
+    B.dp_attention(at, q, H * D, q.shape[0], k, H * D, v, H * D, k.shape[0], y, H * D, None, flags)
+    return y.view(torch.int16)
+
+
+def _inputs(H, D, Mq, Mk, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rnd = lambda n: torch.randn(n, H * D, generator=gen, device="cuda")  # noqa: E731
+    return [(1.5 * rnd(Mq)).to(torch.bfloat16), rnd(Mk).to(torch.bfloat16), rnd(Mk).to(torch.bfloat16)], rnd
+
+
+@pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("causal,biased", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("cap", [0.0])
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_bits_do_not_depend_on_other_sequences(D, cap, causal, biased, flags):
+    """The first sequence's rows stay as they are when the second one's, and the rows behind it, go from zero to scores whose
+    maxima rise from tile to tile."""
+    H = 4
+    slopes = torch.linspace(0.1, 0.003, H, device="cuda") if biased else None
+    for lq, lk in (([600, 90], [600, 90]), ([100, 40], [1000, 40]), ([260, 1], [77, 1])):
+        (q, k, v), rnd = _inputs(H, D, sum(lq) + 70, sum(lk) + 70, 31 + D)
+        out = []
+        for size in (0.0, 12.0):
+            for t, n in ((q, lq[0]), (k, lk[0]), (v, lk[0])):
+                t[n:] = (size * rnd(t.shape[0] - n)).to(torch.bfloat16)
+            out.append(_bits(H, D, lq, lk, q, k, v, causal, cap, slopes, flags)[:lq[0]])
+        assert torch.equal(out[0], out[1]), int((out[0] != out[1]).sum())
+
+
+@pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("cap", [0.0])
+def test_bits_do_not_depend_on_hidden_keys(cap, flags):
+    """Causal mask: keys behind a query go from zero to large ones."""
+    H, D, n, seen = 4, 64, 400, 250
+    (q, k, v), rnd = _inputs(H, D, n, n, 5)
+    out = []
+    for size in (0.0, 12.0):
+        k[seen:] = (size * rnd(n - seen)).to(torch.bfloat16)
+        out.append(_bits(H, D, [n], [n], q, k, v, True, cap, None, flags)[:seen])
+    assert torch.equal(out[0], out[1]), int((out[0] != out[1]).sum())
+
+
+@pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("cap", [0.0])
+def test_bits_do_not_depend_on_other_queries(cap, flags):
+    """A query's row is the same whatever the other queries of its sequence are."""
+    H, D, n = 4, 64, 300
+    (q, k, v), rnd = _inputs(H, D, n, n, 6)
+    out = []
+    for size in (0.0, 12.0):
+        q[1::2] = (size * rnd(n // 2)).to(torch.bfloat16)
+        out.append(_bits(H, D, [n], [n], q, k, v, False, cap, None, flags)[::2])
+    assert torch.equal(out[0], out[1]), int((out[0] != out[1]).sum())
+
+
+def test_every_operand_beyond_32_bit_offsets():
+    """Queries, keys, values and outputs in columns of one buffer of 9 GB whose last sequence starts behind element 2^32."""
+    H, D, ld, M, first = 2, 64, 1 << 20, 4400, 4150
+    assert first * ld > 1 << 32
+    n, W = M - first, H * D
+    buf = torch.empty(M, ld, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    buf[first:, :3 * W] = torch.randn(n, 3 * W, generator=gen, device="cuda").to(torch.bfloat16)
+    q, k, v, y = (buf[:, i * W:] for i in range(4))
+    for nq, flags in ((1, 0), (n, 0), (n, B.DP_FLAG_FORCE_SIMT)):
+        buf[first:, 3 * W:4 * W] = 7.0
+        starts = (torch.tensor([a, M], dtype=torch.int32, device="cuda") for a in (M - nq, first))
+        at = B.make_attn(H, H, D, 1, nq, n, 0.125, q_start=next(starts), k_start=next(starts))
+        B.dp_attention(at, q, ld, M, k, ld, v, ld, M, y, ld, None, flags)
+        a = first + n - nq
+        rows = lambda t, at: t[at:, :W].reshape(M - at, H, D)  # noqa: E731
+        want, tol = R.attention(rows(q, a), rows(k, first), rows(v, first), [nq], [n], rows(y, a), 0.125)
+        assert ((rows(y, a).double() - want).abs() <= tol).all()
+        assert (y[first:a, :W] == 7.0).all()
