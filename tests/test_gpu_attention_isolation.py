@@ -32,11 +32,11 @@ def _inputs(H, D, Mq, Mk, seed):
 
 @pytest.mark.parametrize("flags", FORMS)
 @pytest.mark.parametrize("causal,biased", [(False, False), (True, False), (False, True)])
-@pytest.mark.parametrize("cap", [0.0])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
 @pytest.mark.parametrize("D", [64, 72, 128])
 def test_bits_do_not_depend_on_other_sequences(D, cap, causal, biased, flags):
     """The first sequence's rows stay as they are when the second one's, and the rows behind it, go from zero to scores whose
-    maxima rise from tile to tile."""
+    maxima rise from tile to tile and leave the range of the tanh's polynomial."""
     H = 4
     slopes = torch.linspace(0.1, 0.003, H, device="cuda") if biased else None
     for lq, lk in (([600, 90], [600, 90]), ([100, 40], [1000, 40]), ([260, 1], [77, 1])):
@@ -50,7 +50,7 @@ def test_bits_do_not_depend_on_other_sequences(D, cap, causal, biased, flags):
 
 
 @pytest.mark.parametrize("flags", FORMS)
-@pytest.mark.parametrize("cap", [0.0])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
 def test_bits_do_not_depend_on_hidden_keys(cap, flags):
     """Causal mask: keys behind a query go from zero to large ones."""
     H, D, n, seen = 4, 64, 400, 250
@@ -63,7 +63,7 @@ def test_bits_do_not_depend_on_hidden_keys(cap, flags):
 
 
 @pytest.mark.parametrize("flags", FORMS)
-@pytest.mark.parametrize("cap", [0.0])
+@pytest.mark.parametrize("cap", [0.0, 8.0])
 def test_bits_do_not_depend_on_other_queries(cap, flags):
     """A query's row is the same whatever the other queries of its sequence are."""
     H, D, n = 4, 64, 300
