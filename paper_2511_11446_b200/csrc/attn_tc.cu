@@ -163,7 +163,7 @@ __device__ __forceinline__ float tc_weights(const float (&s)[N], float scale, fl
 // special-function unit, beyond by two operations of it. Which one is decided score by score, so that a result does not depend on the
 // scores beside it (other sequences' queries and keys may be among them); a warp whose scores are all small, as capped scores of real
 // models are, takes polynomials only. (8 x 1024 tokens, 16 heads of 64, most scores beyond: 137 us with one form for a warp's 32 rows, 153 so; within
-the range 98 and 99.)
+// the range 98 and 99.)
 template <int N>
 __device__ __forceinline__ void tc_tanh(float (&s)[N], float two_log2e_k, float k) {
   float top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
