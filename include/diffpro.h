@@ -324,7 +324,8 @@ int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const
  *                 time may use it
  * C a multiple of 8, at most 4608, and of `groups` (at most 1024); x and the output 16-byte aligned, ldx and ldy multiples of
  * 8, ldq of 16; the output does not overlap x; at most 2^31 rows and 2^23 samples. Buffers and stream belong to the current device.
- * Sums of squares have to stay in fp32's range; with eps = 0 a constant group gives NaN (0 / 0). n_samples == 0 or rows == 0 is a no-op.
+ * Sums of squares have to stay in fp32's range; with eps = 0 a constant group gives NaN (0 / 0), and so does a group that holds an
+ * infinity or a NaN (in codes: the scales of all rows of its sample). n_samples == 0 or rows == 0 is a no-op.
  * Errors: DP_ERR_INVALID_ARG, DP_ERR_SHAPE, DP_ERR_ALIGN, DP_ERR_WORKSPACE, DP_ERR_ARCH.
  */
 #define DP_ACT_NONE 0

@@ -213,7 +213,9 @@ __device__ __forceinline__ void gn_groups(const GnArgs& a, const uint16_t* xs, i
       w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
     }
     if (live && k == 0) {
-      const double mean = u * a.inv_n, var = fmax(w * a.inv_n - mean * mean, 0.0);
+      const double mean = u * a.inv_n;
+      double var = w * a.inv_n - mean * mean;
+      if (var < 0.0) var = 0.0;  // (a group that holds an infinity or a NaN keeps its NaN, which fmax would drop)
       const float v = static_cast<float>(var + static_cast<double>(a.eps));
       float r = rsqrtf(v);
       if (v > 1e-30f) r = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);  // (a step of Newton's: the last bits; none where v r^2 would underflow)
