@@ -313,7 +313,7 @@ int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const
  * (the method quantizes those like a DiT's linears; Step 3 keeps normalization in higher precision). x is bf16
  * [n_samples * rows][ldx], `groups` groups of C / groups neighbouring channels; over the rows * C / groups values of a sample's
  * group
- *     mean, var (biased), from fp32 sums of the values less one of them, joined in double
+ *     mean, var (biased), in fp32: sums over short runs less one of their own values, joined as means and squared deviations
  *     h = (x - mean) / sqrt(var + eps) * gamma[c] + beta[c]                        fp32
  *     act(h): DP_ACT_NONE h, DP_ACT_SILU h / (1 + exp(-h))                          fp32
  * dp_group_norm writes y = bf16(act(h)) [n_samples * rows][ldy]; dp_group_norm_daq writes Eq. "daq" of act(h), codes

@@ -7,10 +7,14 @@
 // In front of a U-Net block's projections the paper's method quantizes the activations like any other linear's (Eq. "daq");
 // dp_group_norm_daq writes the codes in the pass that would write y.
 //
-// Statistics first: sums of d and d^2, d = x - pivot with the group's first value as pivot, so that a level far above the spread
-// does not cancel (a constant map gives var = 0 and h = beta exactly). A thread keeps 8 channels of every `lanes`-th row, in fp32
-// over a few hundred values (65536 for a batch of 100 GB); groups' sums of CTAs are added in double, in a fixed order, and give each channel
-//     h = (x - pivot) * a + b,   a = gamma * rstd,   b = beta - (mean - pivot) * a       (x - pivot is exact or nearly so)
+// Statistics first, as means and sums of squared deviations M2, joined like those of samples (Chan, Golub and LeVeque 1979: two have
+// M2 = M2a + M2b + na nb / (na + nb) (mean_a - mean_b)^2), in a fixed order and in fp32. A thread keeps 8 channels of every `lanes`-th row; over
+// runs of 24 rows it sums d and d^2, d = x - the run's first value. That value is one of the run's own, so (it - mean)^2 <= M2: neither a
+// level nor an outlier cancels more than a factor of 25 in the last bits of M2. The same holds for what joins lanes, channels and
+// CTAs about the first of them. (One pivot for the group loses what it is untypical by: level 100, spread 0.5, first value 0, 150 samples of 8192 x
+// 320 gave rstd a tenth off.) Means are held less the group's first value, so that a constant map gives var = 0 and h = beta exactly, and
+// give each channel
+//     h = (x - pivot) * a + b,   a = gamma * rstd,   b = beta - (mean - pivot) * a,   pivot = mean rounded to fp32
 //
 // Bound by memory: 2 bytes in and 2 (or 1) out per element, if x need not be read twice from it. Two forms:
 //  - maps of up to 8 x 64 KB or so a sample: one kernel, a cluster of CTAs to a sample. Each keeps its rows in shared memory while the
@@ -24,8 +28,11 @@ namespace dp {
 
 constexpr int kGnMaxThreads = 640;
 constexpr int kGnSumUnroll = 6, kGnUnroll = 4;                  // rows that a thread adds while as many are in flight
+constexpr int kGnRun = 4 * kGnSumUnroll;                        // rows that it adds about one of them
 constexpr int kGnMaxCluster = 8;               // (16, measured: 8 samples of 64 x 640 12.7 us, 6.5 with 8)
 constexpr size_t kGnSmem = 113 * 1024;          // of a CTA: two to an SM, one of which reads while the other writes
+// (rows in shared memory are one run a thread: more than half of kGnMaxThreads hold 16 bytes of each)
+static_assert(kGnSmem / (16 * (kGnMaxThreads / 2 + 1)) < kGnRun, "rows of a thread in shared memory");
 
 struct GnArgs {
   const uint16_t* x;
@@ -34,23 +41,30 @@ struct GnArgs {
   uint64_t per_inv;    // ceil(2^32 / per): c / per = c * per_inv >> 32 for c < 2^16 (a division takes twenty instructions)
   const uint16_t *gamma, *beta;  // [C] or null
   float eps;
-  double inv_n;        // 1 / values of a group
+  float inv_n, inv_rows;  // 1 / values of a group, of a channel
   uint16_t* y;
   int64_t ldy;
   int8_t* q;
   int64_t ldq;
   float* s_a;
-  float2* sums;  // [sample][chunk][G]
+  float2* sums;  // [sample][chunk][G]: mean less the group's first value, M2
+  int32_t sum_bits, join_bits;  // log2 of the threads that take a group in gn_sums, gn_groups
   int32_t chunks;      // (CTAs of the cluster in the one-kernel form)
   int64_t chunk_rows;
   int32_t out_chunks;  // of the kernel that applies them
   int64_t out_rows;
 };
 
-__device__ __forceinline__ float gn_bf16(const uint16_t* p) {
+__device__ __forceinline__ uint32_t gn_bits(const uint16_t* p) {
   uint16_t v;
   asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p) : "memory");
-  return __uint_as_float(static_cast<uint32_t>(v) << 16);
+  return v;
+}
+__device__ __forceinline__ float gn_bf16(const uint16_t* p) { return __uint_as_float(gn_bits(p) << 16); }
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 // Eight bf16 as four packed fp32 pairs.
 __device__ __forceinline__ void gn_unpack(const uint4& v, uint64_t (&f)[4]) {
@@ -86,13 +100,16 @@ struct GnThread {
   }
 };
 
-// Sums of rows [r0, r1) of a sample (xs) by group into out[G] (shared memory or global); with KEEP the rows go to `rows_at` too.
-// part: [2][lanes][C] floats of shared memory.
+// Mean (less the group's first value) and M2 of rows [r0, r1) of a sample (xs) by group into out[G] (shared memory or global); with KEEP
+// the rows go to `rows_at` too. part: [2][lanes][C] floats of shared memory.
 template <bool KEEP>
 __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, const uint16_t* xs, int64_t r0, int64_t r1, float* part,
                                         uint4* rows_at, float2* out) {
+  const int rows = r1 > r0 ? static_cast<int>(r1 - r0) : 0;
+  const int full = rows / t.lanes, extra = rows - full * t.lanes;  // rows of a lane, lanes with one more
+  const uint64_t minus1 = f32x2_pack(-1.0f, -1.0f);
   if (t.lane < t.lanes) {
-    int n = r1 - r0 > t.lane ? (static_cast<int>(r1 - r0) - t.lane + t.lanes - 1) / t.lanes : 0;  // rows of this thread
+    int n = full + (t.lane < extra);  // rows of this thread
     const uint16_t* xp = xs + (r0 + t.lane) * a.ldx + t.vec * 8;
     uint4* keep = rows_at + t.lane * t.vecs + t.vec;
     const int64_t step = t.lanes * a.ldx;
@@ -101,12 +118,22 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
 #pragma unroll
     for (int u = 0; u < kGnSumUnroll; ++u, xp += step)
       if (u < n) v[u] = ld_global_v4(xp);
-    uint64_t s2[4], ss2[4], minus[4];
+    uint4 base;  // the groups' first values
+    uint32_t* bw = &base.x;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      s2[j] = ss2[j] = 0;
-      minus[j] = f32x2_pack(-gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j) * a.per), -gn_bf16(xs + gn_group(a, t.vec * 8 + 2 * j + 1) * a.per));
-    }
+    for (int j = 0; j < 4; ++j)
+      bw[j] = gn_bits(xs + gn_group(a, t.vec * 8 + 2 * j) * a.per) | gn_bits(xs + gn_group(a, t.vec * 8 + 2 * j + 1) * a.per) << 16;
+    if (n == 0) v[0] = make_uint4(0, 0, 0, 0);  // (counts for nothing)
+    uint64_t s2[4], ss2[4], minus[4];
+    auto begin_run = [&](const uint4& v) {
+      uint64_t f[4];
+      gn_unpack(v, f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        minus[j] = f32x2_mul(f[j], minus1);
+        s2[j] = ss2[j] = 0;
+      }
+    };
     auto add = [&](const uint4& v) {
       uint64_t f[4];
       gn_unpack(v, f);
@@ -117,6 +144,42 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
         ss2[j] = f32x2_fma(d, d, ss2[j]);
       }
     };
+    // A run's mean and M2, joined to those of the `done` rows before it in this thread's own place of `part`; means less the run's first
+    // value, then less what `next` holds: the next run's first value, or the groups'.
+    ulonglong2* means = reinterpret_cast<ulonglong2*>(part + t.lane * a.C + t.vec * 8);
+    ulonglong2* m2s = reinterpret_cast<ulonglong2*>(part + (t.lanes + t.lane) * a.C + t.vec * 8);
+    int done = 0;
+    auto end_run = [&](int run, const uint4& next) {
+      const float inv = rcp_approx(static_cast<float>(max(run, 1)));
+      const uint64_t inv2 = f32x2_pack(inv, inv);
+      uint64_t f[4], mean[4], m2[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mean[j] = f32x2_mul(s2[j], inv2);
+        m2[j] = f32x2_fma(f32x2_mul(s2[j], minus1), mean[j], ss2[j]);
+      }
+      if (!KEEP && done > 0) {
+        const float w = run * rcp_approx(static_cast<float>(done + run));
+        const uint64_t w2 = f32x2_pack(w, w), dw2 = f32x2_pack(done * w, done * w);
+        const ulonglong2 mo[2] = {means[0], means[1]}, qo[2] = {m2s[0], m2s[1]};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t old = j & 1 ? mo[j >> 1].y : mo[j >> 1].x, d = f32x2_fma(old, minus1, mean[j]);
+          mean[j] = f32x2_fma(d, w2, old);
+          m2[j] = f32x2_fma(f32x2_mul(d, d), dw2, f32x2_add(j & 1 ? qo[j >> 1].y : qo[j >> 1].x, m2[j]));
+        }
+      }
+      gn_unpack(next, f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mean[j] = f32x2_fma(f32x2_add(f[j], minus[j]), minus1, mean[j]);
+      means[0] = make_ulonglong2(mean[0], mean[1]);
+      means[1] = make_ulonglong2(mean[2], mean[3]);
+      m2s[0] = make_ulonglong2(m2[0], m2[1]);
+      m2s[1] = make_ulonglong2(m2[2], m2[3]);
+      done += run;
+    };
+    begin_run(v[0]);
+    int run = 0;
     // the next rows are on their way while these are added
     for (; n > 0; n -= kGnSumUnroll) {
       uint4 nx[kGnSumUnroll];
@@ -130,97 +193,123 @@ __device__ __forceinline__ void gn_sums(const GnArgs& a, const GnThread& t, cons
           add(v[u]);
         }
       if constexpr (KEEP) keep += kGnSumUnroll * keep_step;
+      run += min(n, kGnSumUnroll);
+      if constexpr (!KEEP)
+        if (run == kGnRun && n > kGnSumUnroll) {
+          end_run(run, nx[0]);
+          run = 0;
+          begin_run(nx[0]);
+        }
 #pragma unroll
       for (int u = 0; u < kGnSumUnroll; ++u) v[u] = nx[u];
     }
-    float s[8], ss[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f32x2_unpack(s2[j], s[2 * j], s[2 * j + 1]);
-      f32x2_unpack(ss2[j], ss[2 * j], ss[2 * j + 1]);
-    }
-    float4* ps = reinterpret_cast<float4*>(part + t.lane * a.C + t.vec * 8);
-    float4* pss = reinterpret_cast<float4*>(part + (t.lanes + t.lane) * a.C + t.vec * 8);
-    ps[0] = make_float4(s[0], s[1], s[2], s[3]);
-    ps[1] = make_float4(s[4], s[5], s[6], s[7]);
-    pss[0] = make_float4(ss[0], ss[1], ss[2], ss[3]);
-    pss[1] = make_float4(ss[4], ss[5], ss[6], ss[7]);
+    end_run(run, base);
   }
   __syncthreads();
-  // channel by channel over the lanes, in the first lane's place, then group by group
+  // Channel by channel over the lanes, in the first lane's place: blocks of 16 about their first lane's mean, whose distance from the
+  // block's, squared, is at most 16 / rows of the block's M2, are summed and joined. (Two passes, the mean first: 0.3 us more.)
+  const float n_lane = static_cast<float>(full), more = n_lane + 1.0f;
   for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-    float u = 0.0f, w = 0.0f;
-    for (int l = 0; l < t.lanes; ++l) {
-      u += part[l * a.C + c];
-      w += part[(t.lanes + l) * a.C + c];
+    const float *mu = part + c, *m2 = mu + t.lanes * a.C;
+    float n = 0.0f, mean = 0.0f, q = 0.0f;
+    for (int l0 = 0; l0 < t.lanes; l0 += 16) {
+      const int l2 = min(l0 + 16, t.lanes), l1 = min(max(extra, l0), l2);
+      const float ref = mu[l0 * a.C];
+      float u = 0.0f, uu = 0.0f, w = 0.0f;
+#pragma unroll 8
+      for (int l = l0; l < l2; ++l) {
+        const float d = mu[l * a.C] - ref, nd = (l < extra ? more : n_lane) * d;
+        u += nd;
+        uu = fmaf(nd, d, uu);
+        w += m2[l * a.C];
+      }
+      const float nb = more * (l1 - l0) + n_lane * (l2 - l1);
+      if (nb == 0.0f) break;
+      const float ub = u * rcp_approx(nb), qb = w + fmaf(-u, ub, uu), d = ref + ub - mean, share = nb * rcp_approx(n + nb);
+      q += fmaf(d * d, n * share, qb);
+      mean = n > 0.0f ? fmaf(d, share, mean) : d;
+      n += nb;
     }
-    part[c] = u;
-    part[t.lanes * a.C + c] = w;
+    part[c] = mean;
+    part[t.lanes * a.C + c] = q;
   }
   __syncthreads();
-  const float *cu = part, *cw = part + t.lanes * a.C;
-  if (a.per <= 48) {  // a thread to a group
-    for (int g = threadIdx.x; g < a.G; g += blockDim.x) {
-      float u = 0.0f, w = 0.0f;
-      for (int i = 0; i < a.per; ++i) {
-        u += cu[g * a.per + i];
-        w += cw[g * a.per + i];
-      }
-      out[g] = make_float2(u, w);
+  // Then group by group by 2^bits threads. Up to 48 channels about the first one's mean; of more it may be too far from the others: the
+  // mean first.
+  const int bits = a.sum_bits, threads = 1 << bits, at_once = blockDim.x >> bits, in = threadIdx.x & (threads - 1);
+  const float n_rows = static_cast<float>(rows), inv_per = rcp_approx(static_cast<float>(a.per));
+  for (int g0 = 0; g0 < a.G; g0 += at_once) {
+    const int g = g0 + (threadIdx.x >> bits);
+    if ((threadIdx.x & ~31) >> bits >= a.G - g0) break;  // (whole warps)
+    const float *mu = part + min(g, a.G - 1) * a.per, *m2 = mu + t.lanes * a.C;
+    float ref = mu[0], u = 0.0f, uu = 0.0f, w = 0.0f;
+    if (a.per > 48) {
+      for (int i = in; i < a.per; i += threads) u += mu[i] - ref;
+      for (int o = threads >> 1; o > 0; o >>= 1) u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
+      ref = fmaf(u, inv_per, ref);
+      u = 0.0f;
     }
-  } else {  // a warp
-    const int warp = threadIdx.x >> 5, ln = threadIdx.x & 31;
-    for (int g = warp; g < a.G; g += blockDim.x >> 5) {
-      float u = 0.0f, w = 0.0f;
-      for (int i = ln; i < a.per; i += 32) {
-        u += cu[g * a.per + i];
-        w += cw[g * a.per + i];
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
-        w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
-      }
-      if (ln == 0) out[g] = make_float2(u, w);
+    for (int i = in; i < a.per; i += threads) {
+      const float d = mu[i] - ref;
+      u += d;
+      uu = fmaf(d, d, uu);
+      w += m2[i];
     }
+    for (int o = threads >> 1; o > 0; o >>= 1) {
+      u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
+      uu += __shfl_xor_sync(0xFFFFFFFFu, uu, o);
+      w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
+    }
+    if (g < a.G && in == 0) out[g] = make_float2(fmaf(u, inv_per, ref), fmaf(n_rows, fmaf(-u, u * inv_per, uu), w));
   }
 }
 
-// Per group (pivot, mean - pivot, rstd) in shared memory, from the sums of `parts` CTAs: fetch(part, group).
+// Per group (pivot, mean - pivot, rstd) in shared memory, from the means and M2 of `parts` CTAs: fetch(part, group).
 template <typename Fetch>
 __device__ __forceinline__ void gn_groups(const GnArgs& a, const uint16_t* xs, int parts, float* out, Fetch fetch) {
-  // 2^k threads to a group
-  int sub = 1;
-  while (sub < 32 && 2 * sub * a.G <= static_cast<int>(blockDim.x) && sub < parts) sub *= 2;
-  const int step = blockDim.x / sub;
+  const int bits = a.join_bits;  // 2^bits threads to a group
+  const int sub = 1 << bits, step = blockDim.x >> bits;
+  const float chunk_rows = static_cast<float>(a.chunk_rows), n_rows = static_cast<float>(a.rows);
   for (int g0 = 0; g0 < a.G; g0 += step) {  // (the same trips for all threads: shuffles)
-    const int g = g0 + threadIdx.x / sub, k = threadIdx.x % sub;
-    const bool live = g < a.G && static_cast<int>(threadIdx.x) < step * sub;
-    double u = 0.0, w = 0.0;
-    if (live)
-      for (int c = k; c < parts; c += 8 * sub) {
-        float2 v[8];
+    const int g = g0 + (threadIdx.x >> bits), k = threadIdx.x & (sub - 1);
+    const bool live = g < a.G;  // (blockDim.x is a multiple of 32)
+    const float first = live && k == 0 ? gn_bf16(xs + g * a.per) : 0.0f;
+    // About the first part's mean, whose distance from the group's, squared, is at most `parts` / n of M2.
+    float ref = 0.0f, u = 0.0f, uu = 0.0f, w = 0.0f;
+    for (int c = 0; c < parts; c += 8 * sub) {
+      float2 part[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i * sub < parts ? fetch(c + i * sub, g) : make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          u += v[i].x;
-          w += v[i].y;
-        }
+      for (int i = 0; i < 8; ++i) {
+        if (c + i * sub >= parts) break;
+        part[i] = live && c + i * sub + k < parts ? fetch(c + i * sub + k, g) : make_float2(0.0f, 0.0f);
       }
+      if (c == 0) ref = __shfl_sync(0xFFFFFFFFu, part[0].x, threadIdx.x & 31 & ~(sub - 1));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (c + i * sub >= parts) break;
+        // its rows (none behind the last part's; beyond 2^24 rounded, which shifts weights by as little)
+        const float n = fminf(fmaxf(fmaf(static_cast<float>(c + i * sub + k), -chunk_rows, n_rows), 0.0f), chunk_rows);
+        const float d = part[i].x - ref, nd = n * d;
+        u += nd;
+        uu = fmaf(nd, d, uu);
+        w += part[i].y;
+      }
+    }
     for (int o = sub >> 1; o > 0; o >>= 1) {
       u += __shfl_xor_sync(0xFFFFFFFFu, u, o);
+      uu += __shfl_xor_sync(0xFFFFFFFFu, uu, o);
       w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
     }
     if (live && k == 0) {
-      const double mean = u * a.inv_n;
-      double var = w * a.inv_n - mean * mean;
-      if (var < 0.0) var = 0.0;  // (a group that holds an infinity or a NaN keeps its NaN, which fmax would drop)
-      const float v = static_cast<float>(var + static_cast<double>(a.eps));
+      // (a group that holds an infinity or a NaN keeps its NaN, which fmax would drop)
+      const float off = u * a.inv_rows, mean = ref + off, pivot = first + mean;
+      const float var = fmaf(fmaf(-u, off, uu), a.inv_rows, w * a.inv_n), v = (var < 0.0f ? 0.0f : var) + a.eps;
       float r = rsqrtf(v);
       if (v > 1e-30f) r = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);  // (a step of Newton's: the last bits; none where v r^2 would underflow)
-      out[3 * g] = gn_bf16(xs + g * a.per);
-      out[3 * g + 1] = static_cast<float>(mean);
+      out[3 * g] = pivot;
+      // what rounding it has left out (Knuth's sum of two)
+      const float back = pivot - first;
+      out[3 * g + 1] = (first - (pivot - back)) + (mean - back);
       out[3 * g + 2] = r;
     }
   }
@@ -527,15 +616,23 @@ int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, i
                       const void* beta, float eps, bool silu, void* y, int64_t ldy, int8_t* q, int64_t ldq, float* s_a,
                       void* workspace, cudaStream_t stream) {
   GnArgs a{static_cast<const uint16_t*>(x), rows, ldx, C, G, C / G, ((1ull << 32) + C / G - 1) / (C / G), static_cast<const uint16_t*>(gamma),
-           static_cast<const uint16_t*>(beta), eps, 1.0 / (static_cast<double>(rows) * (C / G)), static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
-           static_cast<float2*>(workspace), 0, 0, 0, 0};
+           static_cast<const uint16_t*>(beta), eps, static_cast<float>(1.0 / (static_cast<double>(rows) * (C / G))), static_cast<float>(1.0 / static_cast<double>(rows)), static_cast<uint16_t*>(y), ldy, q, ldq, s_a,
+           static_cast<float2*>(workspace), 0, 0, 0, 0, 0, 0};
   const bool codes = q != nullptr;
   const int threads = gn_threads(C);
   const size_t head = gn_head_bytes(C, G, threads), part = gn_part_bytes(C);
+  // as many as there are, up to a warp and one to `least` channels or parts
+  const auto bits = [G](int32_t of, int least, int of_threads) {
+    int b = 0;
+    while (b < 5 && least << b < of && (2 << b) * G <= of_threads) ++b;
+    return b;
+  };
+  a.sum_bits = bits(C / G, 4, threads);
   cudaError_t e = cudaSuccess;
   if (const int cs = gn_cluster(samples, rows, C, G); cs != 0) {
     a.chunks = cs;
     a.chunk_rows = (rows + cs - 1) / cs;
+    a.join_bits = bits(cs, 1, threads);
     e = launch_cluster(GN_PICK(gn_cluster_kernel, codes, silu), dim3(static_cast<unsigned>(samples * cs)), dim3(threads),
                        head + part + static_cast<size_t>(a.chunk_rows) * C * 2, stream, true, static_cast<unsigned>(cs), a);
   } else {
@@ -548,6 +645,7 @@ int launch_group_norm(const void* x, int64_t samples, int64_t rows, int32_t C, i
     const int out_threads = halves ? gn_threads(C, kGnMaxThreads / 2) : threads;
     a.out_chunks = halves ? gn_chunks(samples, rows, 296) : a.chunks;
     a.out_rows = (rows + a.out_chunks - 1) / a.out_chunks;
+    a.join_bits = bits(a.chunks, 1, out_threads);
     e = launch(gn_stats_kernel, dim3(static_cast<unsigned>(samples * a.chunks)), dim3(threads), part, stream, true, a);
     if (e == cudaSuccess)
       e = launch(GN_PICK(gn_apply_kernel, codes, silu), dim3(static_cast<unsigned>(samples * a.out_chunks)), dim3(out_threads),

@@ -1,4 +1,5 @@
-"""Group normalisation's statistics where they are easily lost: infinities and NaN."""
+"""Group normalisation's statistics where they are easily lost: an untypical first value, levels far above the spread, maps whose
+parts are unlike each other, infinities and NaN."""
 import math
 
 import pytest
@@ -8,16 +9,96 @@ from paper_2511_11446_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 EPS = 1e-5
+U = 2.0 ** -24  # half a step of an fp32 value, relative to it
 
 
 def _ws(n, rows, C, G):
     return torch.full((B.dp_group_norm_workspace(n, rows, C, G),), 0xFF, dtype=torch.uint8, device="cuda")
 
 
+def _want(x, n, rows, C, G, gamma, beta, silu):
+    """One sample of n, [rows, C], in 64 bits: act(h) and the bound of its error before the output's rounding.
+
+    Runs of F = 24 rows of a channel are summed about one of their own values, p. With q = sum (x - p)^2 <= (F + 1) M2 (p is one of
+    the values, so (p - mean)^2 <= M2), a run's M2 is off by (3 F + 12) U q at most and its mean by (F + 3) U sqrt(q / F), 5 (F + 3) U
+    standard deviations. Each of a thread's K runs rounds the mean once more. Then L lanes are joined in blocks of 16, P channels (up
+    to 48, else about their mean) and T parts of the rows, each about the first of them, whose weight is 1 / k of the whole, k = 16, P, T:
+    that costs M2 k times the roundings of a chain of c, (c + 4) U, c = 16, P, T / 8 + 4; and the mean c sqrt(k) U standard
+    deviations. Means are held about the group's first value p0: 8 roundings of |mean - p0|. So, in units of the standard deviation,
+      e = U (5 (F + 3 + K) + L^1.5 + P^1.5 + T^1.5 + 8 m + 16),   m = |mean - p0| / std,
+    is the mean off by, v = U ((3 F + 12) (F + 1) + 16 (16 + 4) + P' (P' + 4) + T (T / 8 + 8)) + 2 e the variance of itself, P' = min(P, 48), and
+    h = gamma z + beta by |gamma| (e + |z| v / 2 + 4 U |z|) + 2 U |beta| and what rounding the mean to fp32 costs, 2 U |mean| / std. The
+    activation multiplies that by 1.1 at most and adds 2^-21 (2 + |h|) of its value."""
+    d = x.double().view(rows, G, C // G)
+    var, mean = torch.var_mean(d, dim=(0, 2), correction=0, keepdim=True)
+    std = torch.sqrt(var + EPS)
+    z = ((d - mean) / std).reshape(rows, C)
+    F, L, P, T = 24, max(1, 640 // (C // 8)), C // G, max(8, min(148 // n, rows // 16 + 1))
+    K, P1 = rows // (T * L * F) + 1, min(P, 48)
+    spread = lambda t: t.expand_as(d).reshape(rows, C)  # noqa: E731
+    m = spread((mean - d[:1, :, :1]).abs() / std)
+    e = U * (5 * (F + 3 + K) + L ** 1.5 + P ** 1.5 + T ** 1.5 + 8 * m + 16)
+    v = U * ((3 * F + 12) * (F + 1) + 16 * 20 + P1 * (P1 + 4) + T * (T / 8 + 8)) + 2 * e
+    g, b = gamma.double(), beta.double()
+    h = z * g + b
+    tol = g.abs() * (e + z.abs() * v / 2 + 4 * U * z.abs() + 2 * U * spread(mean.abs() / std)) + 2 * U * b.abs()
+    if silu:
+        y = h * torch.sigmoid(h)
+        return y, 1.1 * tol + 2.0 ** -21 * (2 + h.abs()) * y.abs()
+    return h, tol
+
+
 def _affine(C, seed):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     return ((1 + 0.3 * torch.randn(C, generator=gen, device="cuda")).to(torch.bfloat16),
             (0.3 * torch.randn(C, generator=gen, device="cuda")).to(torch.bfloat16), gen)
+
+
+def _check(x, n, rows, C, G, gamma, beta, act, samples):
+    y = torch.zeros(n * rows, C, dtype=torch.bfloat16, device="cuda")
+    B.dp_group_norm(x, n, rows, C, C, G, gamma, beta, EPS, act, y, C, _ws(n, rows, C, G))
+    for s in samples:
+        at = slice(s * rows, (s + 1) * rows)
+        want, tol = _want(x[at], n, rows, C, G, gamma, beta, act == B.DP_ACT_SILU)
+        off = (y[at].double() - want).abs() - (tol + 2.0 ** -8 * (want.abs() + tol))
+        assert (off <= 0).all(), (s, float(off.max()), int((off > 0).sum()))
+
+
+SHAPES = [(2, 64, 1280, 32), (1, 2000, 64, 8), (8, 1023, 640, 32), (16, 16384, 320, 32), (150, 8192, 320, 32), (1, 300_001, 64, 32)]
+
+
+@pytest.mark.parametrize("act", [B.DP_ACT_NONE, B.DP_ACT_SILU])
+@pytest.mark.parametrize("level,spread,first", [(100.0, 0.5, 0.0), (0.0, 1.0, 1000.0), (0.0, 1.0, -100.0)])
+@pytest.mark.parametrize("n,rows,C,G", SHAPES)
+def test_untypical_first_values(n, rows, C, G, level, spread, first, act):
+    """A sample's first row is far from all others (a padded corner, an outlier)."""
+    gamma, beta, gen = _affine(C, rows)
+    x = torch.empty(n * rows, C, dtype=torch.bfloat16, device="cuda")
+    for s in range(n):
+        x[s * rows:(s + 1) * rows] = level + spread * torch.randn(rows, C, generator=gen, device="cuda")
+    x[::rows] = first
+    _check(x, n, rows, C, G, gamma, beta, act, {0, n // 2, n - 1})
+
+
+@pytest.mark.parametrize("n,rows,C,G", SHAPES)
+def test_maps_whose_parts_are_unlike(n, rows, C, G):
+    """Level and spread change along the rows: leaving out or taking twice a part of them moves mean and variance."""
+    gamma, beta, gen = _affine(C, rows + 1)
+    t = torch.linspace(0, 1, rows, device="cuda").view(rows, 1)
+    x = torch.empty(n * rows, C, dtype=torch.bfloat16, device="cuda")
+    for s in range(n):
+        x[s * rows:(s + 1) * rows] = 10 * t * t - 3 + (0.3 + 4 * t) * torch.randn(rows, C, generator=gen, device="cuda")
+    _check(x, n, rows, C, G, gamma, beta, B.DP_ACT_NONE, {0, n // 2, n - 1})
+
+
+@pytest.mark.parametrize("every", [1, 7])
+def test_outliers_in_many_rows(every):
+    """Every few rows a channel is far out, the rows that threads begin with among them."""
+    n, rows, C, G = 4, 8000, 320, 32
+    gamma, beta, gen = _affine(C, every)
+    x = torch.randn(n * rows, C, generator=gen, device="cuda")
+    x[::every, ::5] += 300.0
+    _check(x.to(torch.bfloat16), n, rows, C, G, gamma, beta, B.DP_ACT_SILU, range(n))
 
 
 @pytest.mark.parametrize("act", [B.DP_ACT_NONE, B.DP_ACT_SILU])
