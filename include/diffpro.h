@@ -315,7 +315,7 @@ int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const
  * group
  *     mean, var (biased), in fp32: sums over short runs less one of their own values, joined as means and squared deviations
  *     h = (x - mean) / sqrt(var + eps) * gamma[c] + beta[c]                        fp32
- *     act(h): DP_ACT_NONE h, DP_ACT_SILU h / (1 + exp(-h))                          fp32
+ *     act(h): DP_ACT_NONE h, DP_ACT_SILU h / (1 + exp(-h))                          fp32; below h = -43 good to |h| 2^-62
  * dp_group_norm writes y = bf16(act(h)) [n_samples * rows][ldy]; dp_group_norm_daq writes Eq. "daq" of act(h), codes
  * [..][ldq] and a scale per row as dp_daq_quantize, for dp_wq_linear(w, q, ldq, s_a, ...): the normalized values exist only
  * in fp32 then.

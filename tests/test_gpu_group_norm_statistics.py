@@ -128,3 +128,22 @@ def test_groups_with_infinities_are_not_numbers(n, rows, C, G, value, act):
         ok = torch.ones(n, dtype=torch.bool)
         ok[row // rows] = False
         assert s_a[row // rows].isnan().all() and s_a[ok.cuda()].isfinite().all()
+
+
+def test_silu_far_below_zero():
+    """h / (1 + e^-h) to its last bits down to h = -43, and to |h| 2^-62 below."""
+    rows, C, G = 64, 64, 1
+    x = torch.zeros(rows, C, device="cuda")
+    x[:, :32], x[:, 32:] = -1.0, 1.0  # mean 0, variance 1
+    x = x.to(torch.bfloat16)
+    beta = torch.zeros(C, device="cuda")
+    beta[:32] = torch.linspace(-1, -88, 32, device="cuda")
+    beta[32::2] = torch.linspace(-40, -80, 16, device="cuda")  # pairs of a small and a large one
+    gamma, beta = torch.ones(C, dtype=torch.bfloat16, device="cuda"), beta.to(torch.bfloat16)
+    y = torch.zeros(rows, C, dtype=torch.bfloat16, device="cuda")
+    B.dp_group_norm(x, 1, rows, C, C, G, gamma, beta, 0.0, B.DP_ACT_SILU, y, C, _ws(1, rows, C, G))
+    h = x.double() + beta.double()
+    want = h * torch.sigmoid(h)
+    # h is off by 2^-20 at most (its size below 128, four roundings); then as for any other value
+    tol = want.abs() * (2.0 ** -8 + 2.0 ** -20 + 2.0 ** -21 * (2 + h.abs())) + torch.where(h < -42.9, h.abs() * 2.0 ** -62, 0.0)
+    assert ((y.double() - want).abs() <= tol).all(), ((y.double() - want).abs() - tol).max()
