@@ -571,6 +571,15 @@ static bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b
 // Whether `rows` rows `ld` elements apart end within 2^46 elements of their start: beyond every address space, and a product that
 // passes 64 bits would hide an overlap.
 static bool extent_ok(int64_t rows, int64_t ld) { return rows < 2 || ld <= (1ll << 46) / (rows - 1); }
+// Whether rows of `aw` and `bw` bytes, ap and bp bytes apart, meet; columns of one buffer are apart where neither reaches the other within a
+// row.
+static bool rows_overlap(const void* a, int64_t a_bytes, int64_t ap, int64_t aw, const void* b, int64_t b_bytes, int64_t bp, int64_t bw) {
+  if (!ranges_meet(a, a_bytes, b, b_bytes)) return false;
+  if (ap != bp || aw > ap || bw > bp) return true;
+  const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(a));
+  const int64_t off = (d % ap + ap) % ap;
+  return off < aw || off + bw > ap;
+}
 // `rows` x `heads` vectors of D elements of 16 bits.
 struct AttnRange {
   const void* p;
@@ -582,12 +591,7 @@ struct AttnRange {
   int64_t width() const { return (heads - 1) * hs + D; }
 };
 static bool attn_overlap(const AttnRange& a, const AttnRange& b) {
-  if (!ranges_meet(a.p, a.bytes(), b.p, b.bytes())) return false;
-  if (a.ld != b.ld || a.width() > a.ld || b.width() > b.ld) return true;
-  // columns of one buffer: apart where neither reaches the other within a row
-  const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(a.p));
-  const int64_t off = ((d / 2) % a.ld + a.ld) % a.ld;
-  return off < a.width() || off + b.width() > a.ld;
+  return rows_overlap(a.p, a.bytes(), 2 * a.ld, 2 * a.width(), b.p, b.bytes(), 2 * b.ld, 2 * b.width());
 }
 
 extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const void* k, int64_t ldk,
@@ -690,7 +694,7 @@ static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, 
     return fail(DP_ERR_ALIGN, "%s: pointers and pitches must be 16-byte aligned", name);
   if (!workspace || workspace_bytes < group_norm_workspace(n, rows, C, G) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return fail(DP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, 256-byte aligned", name, group_norm_workspace(n, rows, C, G));
-  if (ranges_meet(x, 2 * ((n * rows - 1) * ldx + C), out, out_size * ((n * rows - 1) * ldo + C)))
+  if (rows_overlap(x, 2 * ((n * rows - 1) * ldx + C), 2 * ldx, 2 * C, out, out_size * ((n * rows - 1) * ldo + C), out_size * ldo, out_size * C))
     return fail(DP_ERR_INVALID_ARG, "%s: the output overlaps x", name);
   int st = check_device();
   if (st != DP_OK) return st;

@@ -135,3 +135,9 @@ def test_group_norm_nothing_to_do_and_codes_need_scales():
     assert _gn(True, s_a=None) == B.DP_ERR_INVALID_ARG
     assert _gn(True, s_a=4 * A + 2) == B.DP_ERR_ALIGN
     assert B.dp_group_norm_workspace(2, 10, 64, 8) >= 256 and B.dp_group_norm_workspace(0, 0, 64, 8) >= 256
+
+
+@pytest.mark.parametrize("kw", [dict(out=A + 96), dict(out=A + 128 * 2 + 240), dict(out=A + 16, ldx=256), dict(out=A + 256, ldx=256, ldo=512)])
+def test_group_norm_columns_that_meet(kw):
+    """Rows of one buffer: x's 64 columns and the output's reach each other, or do not have the same pitch."""
+    assert _gn(False, **dict(dict(ldx=128, ldo=128), **kw)) == B.DP_ERR_INVALID_ARG

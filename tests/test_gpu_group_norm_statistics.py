@@ -1,5 +1,5 @@
 """Group normalisation's statistics where they are easily lost: an untypical first value, levels far above the spread, maps whose
-parts are unlike each other, infinities and NaN."""
+parts are unlike each other, infinities and NaN; and outputs beside the inputs."""
 import math
 
 import pytest
@@ -147,3 +147,20 @@ def test_silu_far_below_zero():
     # h is off by 2^-20 at most (its size below 128, four roundings); then as for any other value
     tol = want.abs() * (2.0 ** -8 + 2.0 ** -20 + 2.0 ** -21 * (2 + h.abs())) + torch.where(h < -42.9, h.abs() * 2.0 ** -62, 0.0)
     assert ((y.double() - want).abs() <= tol).all(), ((y.double() - want).abs() - tol).max()
+
+
+def test_outputs_beside_the_inputs():
+    """y, or codes, in columns of x's own rows: nothing overlaps."""
+    n, rows, C, G = 2, 300, 320, 32
+    gamma, beta, gen = _affine(C, 4)
+    buf = torch.randn(n * rows, 2 * C, generator=gen, device="cuda").to(torch.bfloat16)
+    x0 = buf[:, :C].clone()
+    y = torch.zeros(n * rows, C, dtype=torch.bfloat16, device="cuda")
+    B.dp_group_norm(x0, n, rows, C, C, G, gamma, beta, EPS, B.DP_ACT_SILU, y, C, _ws(n, rows, C, G))
+    q, s0, s1 = torch.zeros(n * rows, C, dtype=torch.int8, device="cuda"), *(torch.zeros(n * rows, device="cuda") for _ in range(2))
+    B.dp_group_norm_daq(x0, n, rows, C, C, G, gamma, beta, EPS, B.DP_ACT_SILU, q, C, s0, _ws(n, rows, C, G))
+    B.dp_group_norm(buf, n, rows, C, 2 * C, G, gamma, beta, EPS, B.DP_ACT_SILU, buf[:, C:], 2 * C, _ws(n, rows, C, G))
+    assert torch.equal(buf[:, C:], y) and torch.equal(buf[:, :C], x0)
+    codes = buf.view(torch.int8)  # rows of 4 C bytes, x in the first 2 C
+    B.dp_group_norm_daq(buf, n, rows, C, 2 * C, G, gamma, beta, EPS, B.DP_ACT_SILU, codes[:, 2 * C:], 4 * C, s1, _ws(n, rows, C, G))
+    assert torch.equal(codes[:, 2 * C:3 * C], q) and torch.equal(s0, s1) and torch.equal(buf[:, :C], x0)
