@@ -1,5 +1,5 @@
 """Group normalisation's statistics where they are easily lost: an untypical first value, levels far above the spread, maps whose
-parts are unlike each other, infinities and NaN; and outputs beside the inputs."""
+parts are unlike each other, infinities and NaN; outputs beside the inputs, offsets beyond 32 bits."""
 import math
 
 import pytest
@@ -164,3 +164,23 @@ def test_outputs_beside_the_inputs():
     codes = buf.view(torch.int8)  # rows of 4 C bytes, x in the first 2 C
     B.dp_group_norm_daq(buf, n, rows, C, 2 * C, G, gamma, beta, EPS, B.DP_ACT_SILU, codes[:, 2 * C:], 4 * C, s1, _ws(n, rows, C, G))
     assert torch.equal(codes[:, 2 * C:3 * C], q) and torch.equal(s0, s1) and torch.equal(buf[:, :C], x0)
+
+
+def test_every_operand_beyond_32_bit_offsets():
+    """Rows 2^20 elements apart: the last of x, y and the codes lie behind element 2^32."""
+    n, rows, C, G, ld = 3, 1400, 64, 8, 1 << 20
+    M = n * rows
+    assert (M - 1) * ld > 1 << 32
+    gamma, beta, gen = _affine(C, 5)
+    x0 = torch.randn(M, C, generator=gen, device="cuda").to(torch.bfloat16)
+    y0 = torch.zeros(M, C, dtype=torch.bfloat16, device="cuda")
+    q0, s0, s1 = torch.zeros(M, C, dtype=torch.int8, device="cuda"), *(torch.zeros(M, device="cuda") for _ in range(2))
+    B.dp_group_norm(x0, n, rows, C, C, G, gamma, beta, EPS, B.DP_ACT_SILU, y0, C, _ws(n, rows, C, G))
+    B.dp_group_norm_daq(x0, n, rows, C, C, G, gamma, beta, EPS, B.DP_ACT_SILU, q0, C, s0, _ws(n, rows, C, G))
+    x, y = (torch.empty(M, ld, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x[:, :C] = x0
+    B.dp_group_norm(x, n, rows, C, ld, G, gamma, beta, EPS, B.DP_ACT_SILU, y, ld, _ws(n, rows, C, G))
+    assert torch.equal(y[:, :C], y0)
+    q = y.view(torch.int8)[:, :ld]  # (rows 2 ld bytes apart)
+    B.dp_group_norm_daq(x, n, rows, C, ld, G, gamma, beta, EPS, B.DP_ACT_SILU, q, 2 * ld, s1, _ws(n, rows, C, G))
+    assert torch.equal(q[:, :C], q0) and torch.equal(s0, s1)
