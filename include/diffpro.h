@@ -267,7 +267,8 @@ int dp_ln_modulate_daq(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, co
  *     cap > 0:        t_ij = cap * tanh(t_ij / cap)
  *     slopes:         t_ij -= slopes[h] * |pos(i) - j|
  *     DP_MASK_CAUSAL: key j is visible to query i where j <= pos(i) or j < prefix[s]; DP_MASK_NONE: everywhere
- *     y_i = sum_j w_ij v_j,  w_ij = exp(t_ij) / sum_j exp(t_ij) over the visible keys;  no key visible: y_i = 0
+ *     y_i = sum_j w_ij v_j,  w_ij = exp(t_ij) / sum_j exp(t_ij) over the visible keys;  no key visible, or all at t_ij = -inf:
+ *     y_i = 0
  *
  * Sequences are packed: sequence s has the rows q_start[s] .. q_start[s + 1] - 1 of q and y and k_start[s] .. k_start[s + 1]
  * - 1 of k and v, so documents of one buffer do not see each other. Rows of other sequences, between sequences and behind

@@ -94,3 +94,34 @@ def test_every_operand_beyond_32_bit_offsets():
         want, tol = R.attention(rows(q, a), rows(k, first), rows(v, first), [nq], [n], rows(y, a), 0.125)
         assert ((rows(y, a).double() - want).abs() <= tol).all()
         assert (y[first:a, :W] == 7.0).all()
+
+
+@pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("cap", [0.0, 8.0])
+@pytest.mark.parametrize("n", [20, 300])
+def test_infinite_scores(n, cap, flags):
+    """A row whose visible scores are all -inf has no weight to give and is zero, like one that sees no key; a score of +inf or NaN makes
+    its row NaN (a cap takes infinite scores to its own size); keys at -inf count for nothing."""
+    H, D = 2, 64
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    v = torch.randn(n, H * D, generator=gen, device="cuda").to(torch.bfloat16)
+    q, k = (torch.zeros(n, H * D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q3, k3 = q.view(n, H, D), k.view(n, H, D)
+    k3[:, :, 0], k3[:, :, 1], k3[:n // 2, :, 1] = -1.0, -1.0, 1.0
+    k3[n // 3, :, 2], k3[:, :, 3] = 2.0, -1.0
+    q3[1, :, 0] = math.inf   # every score -inf
+    q3[2, :, 0] = -math.inf  # every score +inf
+    q3[3, :, 1] = math.inf   # the first half +inf, the second -inf
+    q3[4, 0, 3] = math.nan   # head 0 only
+    y = _bits(H, D, [n], [n], q, k, v, False, cap, None, flags).view(torch.bfloat16).view(n, H, D)
+    mean = v.double().view(n, H, D).mean(0)
+    tol = 2.0 ** -6 * v.double().abs().view(n, H, D).mean(0) + 1e-3
+    if cap:
+        for row in (1, 2):
+            assert ((y[row].double() - mean).abs() <= tol).all()
+    else:
+        assert (y[1] == 0).all() and y[2].isnan().all() and y[3].isnan().all()
+    assert y[4, 0].isnan().all()
+    rest = torch.ones(n, H, dtype=torch.bool, device="cuda")
+    rest[1:4], rest[4, 0] = False, False
+    assert ((y.double() - mean).abs() <= tol)[rest].all()
