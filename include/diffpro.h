@@ -289,7 +289,7 @@ typedef struct dp_attn {
   const int32_t* k_start;        /* device: [n_seq + 1], with q_start                                         */
   const int32_t* prefix;         /* device: [n_seq] or NULL (0); DP_MASK_CAUSAL only                          */
   const float* slopes;           /* device: [heads] or NULL (no distance bias)                                */
-  float scale, cap;              /* scale finite, >= 0; cap in [0, 65536], 0: scores are not capped (its tanh is good
+  float scale, cap;              /* scale in [0, 2e38]; cap in [0, 65536], 0: scores are not capped (its tanh is good
                                     to 2^-21 of the cap)                                                      */
   int32_t mask;                  /* DP_MASK_NONE, DP_MASK_CAUSAL                                              */
   int32_t reserved;

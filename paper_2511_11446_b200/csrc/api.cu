@@ -616,8 +616,9 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   if (a->mask != DP_MASK_NONE && a->mask != DP_MASK_CAUSAL) return fail(DP_ERR_INVALID_ARG, "dp_attention: mask=%d", a->mask);
   if (a->prefix != nullptr && a->mask != DP_MASK_CAUSAL)
     return fail(DP_ERR_INVALID_ARG, "dp_attention: a prefix goes with DP_MASK_CAUSAL");
-  if (!(a->scale >= 0.0f) || !(a->scale <= 3.0e38f) || !(a->cap >= 0.0f) || !(a->cap <= 65536.0f))
-    return fail(DP_ERR_INVALID_ARG, "dp_attention: scale=%g must be finite and not negative, cap=%g in [0, 65536]", a->scale, a->cap);
+  // (scale * log2(e) has to be finite: a score of 0 times an infinity would be NaN)
+  if (!(a->scale >= 0.0f) || !(a->scale <= 2.0e38f) || !(a->cap >= 0.0f) || !(a->cap <= 65536.0f))
+    return fail(DP_ERR_INVALID_ARG, "dp_attention: scale=%g must be in [0, 2e38], cap=%g in [0, 65536]", a->scale, a->cap);
   const int64_t qh = a->q_head_stride ? a->q_head_stride : D, kh = a->k_head_stride ? a->k_head_stride : D;
   const int64_t vh = a->v_head_stride ? a->v_head_stride : D, yh = a->y_head_stride ? a->y_head_stride : D;
   constexpr int64_t kMaxStride = 1ll << 38;  // elements: a tensor map's strides stay below 2^40 bytes

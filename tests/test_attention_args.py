@@ -141,3 +141,9 @@ def test_group_norm_nothing_to_do_and_codes_need_scales():
 def test_group_norm_columns_that_meet(kw):
     """Rows of one buffer: x's 64 columns and the output's reach each other, or do not have the same pitch."""
     assert _gn(False, **dict(dict(ldx=128, ldo=128), **kw)) == B.DP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("scale", [2.1e38, 2.5e38, 3.0e38])
+def test_attention_scales_whose_multiple_by_log2e_is_infinite(scale):
+    """(a score of 0 would be NaN)"""
+    assert _call(_attn(scale=scale)) == B.DP_ERR_INVALID_ARG
