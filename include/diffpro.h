@@ -323,7 +323,7 @@ int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const
  *   gamma, beta : device bf16 [C], 16-byte aligned, or both NULL (1 and 0)
  *   workspace   : >= dp_group_norm_workspace(...) bytes, 256-byte aligned, contents undefined before and after; one call at a
  *                 time may use it
- * C a multiple of 8, at most 4608, and of `groups` (at most 1024); x and the output 16-byte aligned, ldx and ldy multiples of
+ * eps finite, >= 0; C a multiple of 8, at most 4608, and of `groups` (at most 1024); x and the output 16-byte aligned, ldx and ldy multiples of
  * 8, ldq of 16; the output does not overlap x; at most 2^31 rows and 2^23 samples. Buffers and stream belong to the current device.
  * Sums of squares have to stay in fp32's range; with eps = 0 a constant group gives NaN (0 / 0), and so does a group that holds an
  * infinity or a NaN (in codes: the scales of all rows of its sample). n_samples == 0 or rows == 0 is a no-op.

@@ -684,7 +684,7 @@ static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, 
   if (G > 1024 || rows > kMaxRows || n > (1 << 23) || n * (rows > 0 ? rows : 1) > kMaxRows)
     return fail(DP_ERR_SHAPE, "%s: n_samples=%lld rows=%lld groups=%d", name, (long long)n, (long long)rows, G);
   if ((gamma == nullptr) != (beta == nullptr)) return fail(DP_ERR_INVALID_ARG, "%s: gamma and beta come together", name);
-  if (!(eps >= 0.0f)) return fail(DP_ERR_INVALID_ARG, "%s: eps must be >= 0", name);
+  if (!(eps >= 0.0f) || !(eps <= 3.0e38f)) return fail(DP_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", name);
   if (act != DP_ACT_NONE && act != DP_ACT_SILU) return fail(DP_ERR_INVALID_ARG, "%s: act=%d", name, act);
   if (n == 0 || rows == 0) return DP_OK;
   if (!x || !out || (out_size == 1 && !s_a)) return fail(DP_ERR_INVALID_ARG, "%s: NULL argument", name);

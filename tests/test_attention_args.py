@@ -147,3 +147,8 @@ def test_group_norm_columns_that_meet(kw):
 def test_attention_scales_whose_multiple_by_log2e_is_infinite(scale):
     """(a score of 0 would be NaN)"""
     assert _call(_attn(scale=scale)) == B.DP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("codes", [False, True])
+def test_group_norm_eps_has_to_be_finite(codes):
+    assert _gn(codes, eps=float("inf")) == B.DP_ERR_INVALID_ARG
