@@ -556,7 +556,7 @@ static cudaError_t launch_at(const AttnParams& p, int64_t units, int64_t tiles, 
 }
 
 static int64_t few_units(const AttnParams& p) {  // blocks of 32 rows of a key head
-  return (static_cast<int64_t>(p.max_q) * (p.H / p.KV) + 31) / 32 * p.KV * p.n_seq;
+  return attn_product(attn_product((static_cast<int64_t>(p.max_q) * (p.H / p.KV) + 31) / 32, p.KV), p.n_seq);
 }
 // Whether the keys are cut over clusters, for blocks of 32 rows: always where there is one, and of more where that makes few units of long
 // contexts, which would leave the tcgen05 kernel's tiles of 128 on few SMs. (From 769 keys on and up to 64 units, 40 of more than 96 columns. 16 heads of
@@ -572,7 +572,7 @@ bool attn_cuts_keys(const AttnParams& p) {
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t rows = static_cast<int64_t>(p.max_q) * (p.H / p.KV);
   const bool few = attn_cuts_keys(p);
-  const int64_t tiles = few ? 0 : (rows + 63) / 64, units = few ? few_units(p) : tiles * p.KV * p.n_seq;
+  const int64_t tiles = few ? 0 : (rows + 63) / 64, units = few ? few_units(p) : attn_product(attn_product(tiles, p.KV), p.n_seq);
   if (units > (few ? 0x7FFFFFFF / kAtMaxSplits : 0x7FFFFFFF) || tiles > 0x7FFFFFFF)
     return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)units);
   const cudaError_t e = p.D <= 32   ? launch_at<32>(p, units, tiles, rows, stream, pdl)

@@ -22,6 +22,10 @@ struct AttnParams {
   int32_t* status;
 };
 
+// a * b of numbers that are not negative, or the largest one where it does not fit: tiles, heads and sequences of a call may be up to
+// 2^31 each.
+static inline int64_t attn_product(int64_t a, int64_t b) { return b != 0 && a > INT64_MAX / b ? INT64_MAX : a * b; }
+
 #ifdef __CUDACC__
 
 constexpr float kLog2e = 1.4426950408889634f;

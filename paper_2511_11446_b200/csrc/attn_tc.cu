@@ -850,13 +850,13 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   // Items of 256 queries share K and V between two tiles and hide one's products behind the other's exponentials; of 128, whose
   // keys the warpgroups share, where that many more SMs get work.
   c.rows = 2 * kTcTile;
-  if ((static_cast<int64_t>(p.max_q) + 255) / 256 * pairs * 2 <= sms || p.max_q <= kTcTile) c.rows = kTcTile;
+  if (attn_product((static_cast<int64_t>(p.max_q) + 255) / 256, pairs) <= sms / 2 || p.max_q <= kTcTile) c.rows = kTcTile;
   // From 385 keys on the second warpgroup, idle otherwise, takes every other tile of the keys of 128 queries (one sequence of 256 queries, 16 heads
   // of 72, over 256 / 512 / 1000 / 4096 keys: 9.1 / 12.1 / 17.3 / 50.4 us -> 9.2 / 11.6 / 15.3 / 39.9; 64 of 96, over 96 / 200 / 512: 21.1 / 41.4 / 62.7
   // -> 23.9 / 43.1 / 58.4).
   c.cut = c.rows == kTcTile && p.max_k > 384;
   const int64_t tiles = (static_cast<int64_t>(p.max_q) + c.rows - 1) / c.rows;
-  if (tiles * pairs > 0x7FFFFFFF) return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)(tiles * pairs));
+  if (attn_product(tiles, pairs) > 0x7FFFFFFF) return fail(DP_ERR_SHAPE, "attention: %lld tiles of queries", (long long)attn_product(tiles, pairs));
   c.tiles = static_cast<int32_t>(tiles);
   c.items = static_cast<int32_t>(tiles * pairs);
   // Of equal sequences without a mask all items are alike and a pair's stand together, for its K and V in L2; else 64 pairs, so that
