@@ -41,6 +41,7 @@ constexpr int kMaxDevices = 64;
 struct DeviceInfo {
   int status;  // DP_OK or DP_ERR_ARCH
   int num_sms, max_pairs, max_clusters[kMaxSplits + 1];
+  AttnLimits attn;
 };
 static DeviceInfo g_dev[kMaxDevices];
 static std::atomic<int> g_dev_ready[kMaxDevices];
@@ -60,7 +61,7 @@ int check_device() {
   if (!g_dev_ready[dev].load(std::memory_order_acquire)) {
     std::lock_guard<std::mutex> lock(g_dev_mutex);
     if (!g_dev_ready[dev].load(std::memory_order_relaxed)) {
-      DeviceInfo d = {DP_OK, 0, 0, {}};
+      DeviceInfo d = {DP_OK, 0, 0, {}, {}};
       int major = 0;
       cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
       if (e != cudaSuccess) return fail(DP_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
@@ -68,6 +69,7 @@ int check_device() {
         d.status = DP_ERR_ARCH;
       } else {  // a failure here is reported and NOT cached: the next call tries again
         st = gemm_init_device(dev, &d.num_sms, &d.max_pairs, d.max_clusters);
+        if (st == DP_OK) st = attn_init_device(&d.attn);
         if (st != DP_OK) return st;
       }
       g_dev[dev] = d;
@@ -91,6 +93,11 @@ int num_sms() {
 int gemm_max_pairs() {
   const DeviceInfo* d = ready_device();
   return d ? d->max_pairs : 0;
+}
+
+const AttnLimits* attn_limits() {
+  const DeviceInfo* d = ready_device();
+  return d ? &d->attn : nullptr;
 }
 
 GemmLimits gemm_limits() {

@@ -16,7 +16,7 @@
 namespace dp {
 
 constexpr int kAtThreads = 128, kAtKeys = 64;
-constexpr int kAtMaxSplits = 8;  // CTAs of a cluster
+constexpr int kAtMaxSplits = kAttnMaxSplits;  // CTAs of a cluster
 // Keys of a stage of a warp's ring, and stages: two CTAs to an SM. Small stages cost more arithmetic a key, so they are taken only where they
 // overlap what else would wait (8 sequences of 8192 keys, 4 key heads of 128, one query: 32.9 us by one stage of 32, 28.2 by three of 16; seven
 // queries, two blocks of rows: 44.4 / 45.3).
@@ -487,12 +487,10 @@ constexpr size_t at_few_smem() {
   constexpr size_t join = (W + 1) * static_cast<size_t>(16 * MB) * (DP + 4) * 4;
   return ring > join ? ring : join;
 }
-// Clusters of 1 .. 8 CTAs that a device holds at once (a cluster stays within a group of 16 to 18 SMs), found when it is first used;
-// devices of one architecture have the same.
+constexpr int at_width(int dp) { return dp == 32 ? 0 : dp == 64 ? 1 : dp == 80 ? 2 : dp == 96 ? 3 : 4; }  // of AttnLimits
+// The clusters of 1 .. 8 CTAs that the device holds at once (a cluster stays within a group of 16 to 18 SMs).
 template <int DP, int MB, int W>
-static int g_few_fit[kAtMaxSplits + 1];
-template <int DP, int MB, int W>
-static cudaError_t at_few_init() {
+static cudaError_t at_few_init(AttnLimits* limits) {
   cudaError_t e = cudaFuncSetAttribute(attn_few_kernel<DP, MB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(at_few_smem<DP, MB, W>()));
   for (int splits = 1; splits <= kAtMaxSplits && e == cudaSuccess; ++splits) {
@@ -507,25 +505,25 @@ static cudaError_t at_few_init() {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&g_few_fit<DP, MB, W>[splits], attn_few_kernel<DP, MB, W>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(&limits->few[at_width(DP)][MB - 1][W == 8][splits], attn_few_kernel<DP, MB, W>, &cfg);
   }
   return e;
 }
 template <int DP>
-static int at_init() {
+static int at_init(AttnLimits* limits) {
   DP_CUDA_OK(cudaFuncSetAttribute(attn_rows_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(at_rows_smem<DP>())));
-  DP_CUDA_OK((at_few_init<DP, 1, 4>()));
-  DP_CUDA_OK((at_few_init<DP, 2, 4>()));
-  DP_CUDA_OK((at_few_init<DP, 1, 8>()));
-  DP_CUDA_OK((at_few_init<DP, 2, 8>()));
+  DP_CUDA_OK((at_few_init<DP, 1, 4>(limits)));
+  DP_CUDA_OK((at_few_init<DP, 2, 4>(limits)));
+  DP_CUDA_OK((at_few_init<DP, 1, 8>(limits)));
+  DP_CUDA_OK((at_few_init<DP, 2, 8>(limits)));
   return DP_OK;
 }
-int attn_init_device() {
-  int st = at_init<32>();
-  if (st == DP_OK) st = at_init<64>();
-  if (st == DP_OK) st = at_init<80>();
-  if (st == DP_OK) st = at_init<96>();
-  if (st == DP_OK) st = at_init<128>();
+int attn_init_device(AttnLimits* limits) {
+  int st = at_init<32>(limits);
+  if (st == DP_OK) st = at_init<64>(limits);
+  if (st == DP_OK) st = at_init<80>(limits);
+  if (st == DP_OK) st = at_init<96>(limits);
+  if (st == DP_OK) st = at_init<128>(limits);
   return st;
 }
 
@@ -536,7 +534,8 @@ static cudaError_t launch_few(const AttnParams& p, int64_t units, int row_blocks
   // to each of 80, which fit, 39.1 us, by two 51.2.)
   const int64_t tiles_of_keys = (static_cast<int64_t>(p.max_k) + 31) / 32;
   int splits = static_cast<int>(tiles_of_keys / W < kAtMaxSplits ? tiles_of_keys / W : kAtMaxSplits);
-  while (splits > 1 && g_few_fit<DP, MB, W>[splits] < units) --splits;
+  const AttnLimits* limits = attn_limits();
+  while (splits > 1 && limits != nullptr && limits->few[at_width(DP)][MB - 1][W == 8][splits] < units) --splits;
   splits = splits < 1 ? 1 : splits;
   return launch_cluster(attn_few_kernel<DP, MB, W>, dim3(static_cast<unsigned>(units * splits)), dim3(32 * W), at_few_smem<DP, MB, W>(),
                         stream, pdl, static_cast<unsigned>(splits), p, splits, row_blocks);

@@ -56,7 +56,13 @@ int group_norm_init_device();
 struct AttnParams;
 int launch_attn_rows(const AttnParams& p, cudaStream_t stream, bool pdl);
 bool attn_cuts_keys(const AttnParams& p);  // whether it cuts the keys over clusters of CTAs, for few queries
-int attn_init_device();
+// Clusters of s CTAs of its form for few queries that a device holds at once: [width][blocks of 16 rows - 1][eight warps][s].
+constexpr int kAttnMaxSplits = 8;
+struct AttnLimits {
+  int32_t few[5][2][2][kAttnMaxSplits + 1];
+};
+int attn_init_device(AttnLimits* limits);
+const AttnLimits* attn_limits();  // of the current device, null before check_device()
 // attn_tc.cu -- attention, tcgen05 tiles of 128 queries
 int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl);
 int attn_tc_init_device();

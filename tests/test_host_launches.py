@@ -81,3 +81,18 @@ def test_more_tiles_than_a_grid_are_refused(fake, kw, flags):
     """(also where their number does not fit 64 bits)"""
     assert _attention(fake, dim=8, packed=True, Mq=1, Mk=1, flags=flags, **kw) == B.DP_ERR_SHAPE
     assert _launches(fake) == []
+
+
+def test_each_device_has_its_own_room_for_clusters(fake):
+    """What another device holds at once, asked when that one is first used, does not change a device's grids (and with them the order
+    in which keys are summed)."""
+    fake.fake_set_fit(1, 20)
+    grids = []
+    for device in (0, 1, 0, 1):
+        fake.fake_set_device(device)
+        assert _attention(fake, n_seq=4, max_k=8192) == B.DP_OK
+        (name, grid, _, cluster, *_), = _launches(fake)
+        assert "attn_few_kernel" in name
+        grids.append((grid, cluster))
+    assert grids[0] == grids[2] and grids[1] == grids[3]
+    assert grids[0][1] > grids[1][1]
