@@ -41,7 +41,6 @@ constexpr int kMaxDevices = 64;
 struct DeviceInfo {
   int status;  // DP_OK or DP_ERR_ARCH
   int num_sms, max_pairs, max_clusters[kMaxSplits + 1];
-  AttnLimits attn;
 };
 static DeviceInfo g_dev[kMaxDevices];
 static std::atomic<int> g_dev_ready[kMaxDevices];
@@ -61,7 +60,7 @@ int check_device() {
   if (!g_dev_ready[dev].load(std::memory_order_acquire)) {
     std::lock_guard<std::mutex> lock(g_dev_mutex);
     if (!g_dev_ready[dev].load(std::memory_order_relaxed)) {
-      DeviceInfo d = {DP_OK, 0, 0, {}, {}};
+      DeviceInfo d = {DP_OK, 0, 0, {}};
       int major = 0;
       cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
       if (e != cudaSuccess) return fail(DP_ERR_CUDA, "cudaDeviceGetAttribute: %s", cudaGetErrorString(e));
@@ -69,7 +68,6 @@ int check_device() {
         d.status = DP_ERR_ARCH;
       } else {  // a failure here is reported and NOT cached: the next call tries again
         st = gemm_init_device(dev, &d.num_sms, &d.max_pairs, d.max_clusters);
-        if (st == DP_OK) st = attn_init_device(&d.attn);
         if (st != DP_OK) return st;
       }
       g_dev[dev] = d;
@@ -95,9 +93,37 @@ int gemm_max_pairs() {
   return d ? d->max_pairs : 0;
 }
 
+// The operators between the linears prepare their kernels (65 of them, with their occupancies) on their own first call on a device,
+// in the same way: who runs linears alone does not wait for that.
+static std::atomic<int> g_attn_ready[kMaxDevices], g_norm_ready[kMaxDevices];
+static AttnLimits g_attn_limits[kMaxDevices];
+template <typename Init>
+static int first_use(std::atomic<int> (&ready)[kMaxDevices], Init init) {
+  int st = check_device(), dev = 0;
+  if (st == DP_OK) st = current_device(&dev);
+  if (st != DP_OK || ready[dev].load(std::memory_order_acquire)) return st;
+  std::lock_guard<std::mutex> lock(g_dev_mutex);
+  if (ready[dev].load(std::memory_order_relaxed)) return DP_OK;
+  st = init(dev);
+  if (st == DP_OK) ready[dev].store(1, std::memory_order_release);
+  return st;
+}
+static int check_attn_device() {
+  return first_use(g_attn_ready, [](int dev) {
+    AttnLimits limits{};
+    int st = attn_init_device(&limits);
+    if (st == DP_OK) st = attn_tc_init_device();
+    g_attn_limits[dev] = limits;
+    return st;
+  });
+}
+static int check_norm_device() {
+  return first_use(g_norm_ready, [](int) { return group_norm_init_device(); });
+}
 const AttnLimits* attn_limits() {
-  const DeviceInfo* d = ready_device();
-  return d ? &d->attn : nullptr;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
+  return g_attn_ready[dev].load(std::memory_order_acquire) ? &g_attn_limits[dev] : nullptr;
 }
 
 GemmLimits gemm_limits() {
@@ -647,7 +673,7 @@ extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_
   const AttnRange yr{y, Mq, ldy, H, yh, D};
   if (attn_overlap({q, Mq, ldq, H, qh, D}, yr) || attn_overlap({k, Mk, ldk, KV, kh, D}, yr) || attn_overlap({v, Mk, ldv, KV, vh, D}, yr))
     return fail(DP_ERR_INVALID_ARG, "dp_attention: y overlaps an input");
-  int st = check_device();
+  int st = check_attn_device();
   if (st != DP_OK) return st;
   AttnParams p{};
   p.q = static_cast<const uint16_t*>(q);
@@ -704,7 +730,7 @@ static int group_norm(const char* name, const void* x, int64_t n, int64_t rows, 
     return fail(DP_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, 256-byte aligned", name, group_norm_workspace(n, rows, C, G));
   if (rows_overlap(x, 2 * ((n * rows - 1) * ldx + C), 2 * ldx, 2 * C, out, out_size * ((n * rows - 1) * ldo + C), out_size * ldo, out_size * C))
     return fail(DP_ERR_INVALID_ARG, "%s: the output overlaps x", name);
-  int st = check_device();
+  int st = check_norm_device();
   if (st != DP_OK) return st;
   return launch_group_norm(x, n, rows, C, ldx, G, gamma, beta, eps, act == DP_ACT_SILU, out_size == 2 ? out : nullptr, ldo,
                            out_size == 1 ? static_cast<int8_t*>(out) : nullptr, ldo, s_a, workspace,

@@ -62,7 +62,7 @@ struct AttnLimits {
   int32_t few[5][2][2][kAttnMaxSplits + 1];
 };
 int attn_init_device(AttnLimits* limits);
-const AttnLimits* attn_limits();  // of the current device, null before check_device()
+const AttnLimits* attn_limits();  // of the current device, null before its first dp_attention
 // attn_tc.cu -- attention, tcgen05 tiles of 128 queries
 int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl);
 int attn_tc_init_device();

@@ -413,10 +413,6 @@ int gemm_init_device(int dev, int* num_sms_out, int* max_pairs_out, int* max_clu
   if (st != DP_OK) return st;
   st = gemm_plan_init_device();
   if (st != DP_OK) return st;
-  st = group_norm_init_device();
-  if (st != DP_OK) return st;
-  st = attn_tc_init_device();
-  if (st != DP_OK) return st;
   *num_sms_out = sms;
   *max_pairs_out = pairs;
   return DP_OK;

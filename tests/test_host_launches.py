@@ -96,3 +96,24 @@ def test_each_device_has_its_own_room_for_clusters(fake):
         grids.append((grid, cluster))
     assert grids[0] == grids[2] and grids[1] == grids[3]
     assert grids[0][1] > grids[1][1]
+
+
+def _group_norm(L, codes):
+    n = (1, 4096, 320, 320, 32, None, None, 1e-5, 0, 2 * A, 320)
+    return L.dp_group_norm_daq(A, *n, 3 * A, 4 * A, 1 << 20, None) if codes else L.dp_group_norm(A, *n, 4 * A, 1 << 20, None)
+
+
+def test_operators_prepare_their_kernels_on_their_own_first_call(fake):
+    """Linears and their quantization do not wait for attention and group normalisation; each is prepared on every device that it is
+    called on, once."""
+    prepared = lambda d: [fake.fake_prepared(d, part) for part in (b"attn_", b"gn_")]  # noqa: E731
+    for device in (0, 2):
+        fake.fake_set_device(device)
+        assert fake.dp_daq_quantize(A, 64, 1152, 1152, 2 * A, 1152, 3 * A, None, None) == B.DP_OK
+        assert prepared(device) == [0, 0]
+        assert _group_norm(fake, False) == B.DP_OK and _group_norm(fake, True) == B.DP_OK
+        assert prepared(device)[0] == 0 and prepared(device)[1] > 0
+        assert _attention(fake) == B.DP_OK and _attention(fake, n_seq=9, max_q=300, max_k=300) == B.DP_OK
+        assert min(prepared(device)) > 0
+        for name, _, _, _, smem, allowed, at in _launches(fake):
+            assert at == device and (smem <= 48 << 10 or smem <= allowed), name
