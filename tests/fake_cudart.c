@@ -50,6 +50,7 @@ unsigned __cudaPushCallConfiguration(dim3 g, dim3 b, size_t s, void* st) { (void
 cudaError_t __cudaPopCallConfiguration(dim3* g, dim3* b, size_t* s, void* st) { (void)g, (void)b, (void)s, (void)st; return cudaSuccess; }
 
 cudaError_t cudaGetDevice(int* d) { *d = g_device; return cudaSuccess; }
+cudaError_t cudaSetDevice(int d) { g_device = d; return cudaSuccess; }
 cudaError_t cudaDeviceGetAttribute(int* v, enum cudaDeviceAttr a, int d) {
   *v = a == cudaDevAttrComputeCapabilityMajor ? 10 : a == cudaDevAttrMultiProcessorCount ? g_sms[d] : 0;
   return cudaSuccess;
