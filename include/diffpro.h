@@ -568,7 +568,8 @@ int dp_pack_weights_host(const int8_t* w, int32_t N, int32_t K, int32_t bits, vo
  * bounded wait on it runs out (about 0.15 s), every role of the CTA leaves its loop, tensor memory is
  * freed, the kernel exits normally and `device_status` of that call reads DP_ERR_TIMEOUT; the
  * outputs of the call are undefined. The hook clears itself when that launch is made; k_block < 0
- * clears it without a launch. Host state is per thread.
+ * clears it without a launch. Host state is per thread. If the thread's next such launch is dp_attention's
+ * tcgen05 kernel, `k_block` counts the tiles of K (even) and V (odd) of each CTA's first work item instead.
  */
 void dp_debug_skip_stage_load(int32_t k_block);
 

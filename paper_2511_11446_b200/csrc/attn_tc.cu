@@ -60,6 +60,7 @@ struct AttnTcSched {
   int32_t items;       // tiles * heads * sequences
   int32_t group;       // (sequence, head) pairs whose items are taken together, longest ones first
   int64_t budget;      // cycles that a wait may take
+  int32_t skip;        // test hook (dp_debug_skip_stage_load): copy of a CTA's first item that is left out, or -1
   int32_t sorted;      // sequences by their keys instead, and no items that are not there (up to kTcSorted packed sequences)
 };
 
@@ -469,6 +470,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
       Ring st;
       bool ok = true;
       uint32_t items[2] = {0, 0};
+      int skip = c.skip;
       TcItem it;
       const uint32_t group = p.H / p.KV;
       auto load_q = [&](int t) {
@@ -485,6 +487,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         const int kvh = it.head / group;
         for (int j = 0; j < 2 * n && ok; ++j) {  // K, V, K, V, ..
           if (!(ok = tc_wait(&empty[st.s], st.ph ^ 1u, abort_flag, c.budget))) break;
+          if (j == skip) {  // (nothing is issued for this stage, and nobody completes its barrier)
+            st.next(NS);
+            continue;
+          }
           mbar_arrive_expect_tx(&full[st.s], F::kKvBytes);
 #pragma unroll
           for (int b = 0; b < NBLK; ++b)
@@ -493,6 +499,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
           st.next(NS);
           if (j == 0 && it.n1 > 0) load_q(1);
         }
+        skip = -1;
       }
       if (!ok) producer_drain();
     } else if (warp == 11) {
@@ -592,6 +599,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
         // the rest of the item's tiles is the other tile's: passed on as they come
         pass_on(2 * (n_all - (CUT && n > 0 ? 2 * n - 1 + t : n)));
       }
+      // Products still in flight get a bounded time to end, before tensor memory is given back under them; so do copies in flight where the
+      // loads' thread is already done.
+      if (!ok) producer_drain();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcRegsSoftmax));
@@ -867,6 +877,7 @@ int launch_attn_tc(const AttnParams& p, cudaStream_t stream, bool pdl) {
   const int64_t group = p.causal || p.q_start != nullptr ? 64 : 1;
   c.group = static_cast<int32_t>(group < pairs ? group : pairs);
   const unsigned ctas = static_cast<unsigned>(c.items < sms ? c.items : sms);
+  c.skip = take_debug_skip();
   // Six items of the most keys there can be, at 8192 cycles a tile (2500 or so are usual), and the items that may not be there,
   // 4096 cycles (800) to 32 of them, on top of the library's usual limit.
   c.budget = kWaitBudgetCycles + 6 * 8192 * (p.Mk / 80 + 1) + 4096 * (c.items / (32ll * ctas) + 1);

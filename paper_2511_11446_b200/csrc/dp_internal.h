@@ -182,6 +182,7 @@ int gemm_encode_w(CUtensorMap* out, const void* qweight, int32_t N, int32_t K, i
                   int32_t bn, int32_t cg);
 int launch_gemm(const GemmProblem& p, cudaStream_t stream, bool pdl);
 void gemm_debug_skip_stage_load(int32_t kb);  // see dp_debug_skip_stage_load
+int32_t take_debug_skip();                    // its value, which is cleared
 // Two ranges (a plan's next layer's packed weights and its bf16 input) that the calling thread's next
 // tensor-core launch sends on their way into L2 while it runs; cleared by that launch. Hints: any valid
 // device ranges of the caller's, or nullptr.

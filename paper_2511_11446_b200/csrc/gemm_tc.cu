@@ -606,9 +606,14 @@ NextReads take_next_reads(unsigned ctas) {
   return n;
 }
 
-// dp_debug_skip_stage_load: consumed by the calling thread's next single-CTA 8-bit launch.
+// dp_debug_skip_stage_load: consumed by the calling thread's next single-CTA 8-bit launch, or attn_tc_kernel's.
 static thread_local int32_t g_skip_kb = -1;
 void gemm_debug_skip_stage_load(int32_t kb) { g_skip_kb = kb < 0 ? -1 : kb; }
+int32_t take_debug_skip() {
+  const int32_t kb = g_skip_kb;
+  g_skip_kb = -1;
+  return kb;
+}
 
 int launch_gemm(const GemmProblem& g, cudaStream_t stream, bool pdl) {
   if (g.M == 0) return DP_OK;
@@ -616,8 +621,7 @@ int launch_gemm(const GemmProblem& g, cudaStream_t stream, bool pdl) {
   const int cg = g.cg == 2 ? 2 : 1;
   GemmParams p;
   if (cg == 1 && g.bits == 8) {
-    p.dbg_skip_kb = g_skip_kb;
-    g_skip_kb = -1;
+    p.dbg_skip_kb = take_debug_skip();
   }
   p.s_a = g.s_a;
   p.s_w = g.s_w;
