@@ -184,3 +184,16 @@ def test_every_operand_beyond_32_bit_offsets():
     q = y.view(torch.int8)[:, :ld]  # (rows 2 ld bytes apart)
     B.dp_group_norm_daq(x, n, rows, C, ld, G, gamma, beta, EPS, B.DP_ACT_SILU, q, 2 * ld, s1, _ws(n, rows, C, G))
     assert torch.equal(q[:, :C], q0) and torch.equal(s0, s1)
+
+
+@pytest.mark.parametrize("size", [1.0, 1e12, 1e-8])
+@pytest.mark.parametrize("n,rows,C,G", [(1, 5000, 8, 1), (2, 3000, 24, 3), (1, 900, 1024, 1024), (3, 700, 4608, 4), (2, 1, 64, 4), (1, 13, 64, 8),
+                                        (400, 40, 72, 9), (7, 401, 2304, 1)])
+def test_untypical_values_at_odd_shapes(n, rows, C, G, size):
+    """One lane or 640 of them, one group or as many as channels, fewer rows than lanes, CTAs without rows; large and small numbers."""
+    gamma, beta, gen = _affine(C, rows + C)
+    x = torch.randn(n * rows, C, generator=gen, device="cuda") + 30
+    x[::rows] = -200.0
+    x[n * rows // 2, C // 2] = 900.0
+    x = (x * size).to(torch.bfloat16)
+    _check(x, n, rows, C, G, gamma, beta, B.DP_ACT_NONE, range(min(n, 5)))
