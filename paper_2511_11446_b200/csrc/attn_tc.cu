@@ -671,7 +671,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ C
           m = top;
         } else if (__any_sync(0xFFFFFFFFu, top > m + kTcRise)) {
           if (!product_before()) break;
-          // (only rows whose own maximum has: the warp's others may be queries of another sequence, or nobody's)
+          // Only rows whose own maximum has: the warp's others may be queries of another sequence, or nobody's. (8192 tokens causal with distance
+          // bias, whose maxima rise with the keys: 364 us with all rows of the warp at once, 370 so.)
           const float to_m = top > m + kTcRise ? top : m, f = to_m == -INFINITY ? 1.0f : ex2(m - to_m);
           m = to_m;
           l *= f;
