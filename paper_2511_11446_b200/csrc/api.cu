@@ -93,7 +93,7 @@ int gemm_max_pairs() {
   return d ? d->max_pairs : 0;
 }
 
-// The operators between the linears prepare their kernels (65 of them, with their occupancies) on their own first call on a device,
+// The operators between the linears prepare their kernels (61 of them, with their occupancies) on their own first call on a device,
 // in the same way: who runs linears alone does not wait for that.
 static std::atomic<int> g_attn_ready[kMaxDevices], g_norm_ready[kMaxDevices];
 static AttnLimits g_attn_limits[kMaxDevices];

@@ -37,6 +37,7 @@ def fake(fake_path, tmp_path):
     with open(fake_path, "rb") as f, open(so, "wb") as g:
         g.write(f.read())
     L = C.CDLL(so)
+    os.remove(so)  # (mapped; a copy for every test takes room)
     for name in ("dp_attention", "dp_group_norm", "dp_group_norm_daq", "dp_daq_quantize", "dp_group_norm_workspace"):
         getattr(L, name).argtypes = getattr(B.lib(), name).argtypes
     L.dp_group_norm_workspace.restype = C.c_size_t
