@@ -624,7 +624,17 @@ struct AttnRange {
   int64_t width() const { return (heads - 1) * hs + D; }
 };
 static bool attn_overlap(const AttnRange& a, const AttnRange& b) {
-  return rows_overlap(a.p, a.bytes(), 2 * a.ld, 2 * a.width(), b.p, b.bytes(), 2 * b.ld, 2 * b.width());
+  if (!rows_overlap(a.p, a.bytes(), 2 * a.ld, 2 * a.width(), b.p, b.bytes(), 2 * b.ld, 2 * b.width())) return false;
+  // heads that alternate in one buffer: with the same strides, vector by vector over the distances between two rows and two heads
+  if (a.ld != b.ld || (a.heads > 1 && b.heads > 1 && a.hs != b.hs) || a.heads > 1024 || b.heads > 1024) return true;
+  const int64_t hs = a.heads > 1 ? a.hs : b.hs, rows = a.rows > b.rows ? a.rows : b.rows;
+  const int64_t d = (static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p)) - static_cast<int64_t>(reinterpret_cast<uintptr_t>(a.p))) / 2;
+  for (int64_t h = 1 - b.heads; h < a.heads; ++h) {
+    // vector at d = h hs + r ld + (less than D either way)
+    const int64_t left = d - h * hs, r = left >= 0 ? left / a.ld : -((-left + a.ld - 1) / a.ld), off = left - r * a.ld;  // 0 <= off < ld
+    if ((off < a.D && r > -rows && r < rows) || (a.ld - off < a.D && r + 1 > -rows && r + 1 < rows)) return true;
+  }
+  return false;
 }
 
 extern "C" int dp_attention(const dp_attn* a, const void* q, int64_t ldq, int64_t Mq, const void* k, int64_t ldk,

@@ -152,3 +152,13 @@ def test_attention_scales_whose_multiple_by_log2e_is_infinite(scale):
 @pytest.mark.parametrize("codes", [False, True])
 def test_group_norm_eps_has_to_be_finite(codes):
     assert _gn(codes, eps=float("inf")) == B.DP_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("y", [A + 64 * 2, A + 128 * 2 + 16, A + 256 * 2 + 64 * 2, A + (19 * 1024 + 3 * 256 + 32) * 2])
+def test_attention_heads_of_one_buffer_that_meet(y):
+    """Rows of 4 heads x 4 vectors of 64: q, k, v and y alternate. y on k's vectors, reaching from v's into its own, on another head's k, and
+    in the last vector of q."""
+    kw = dict(ldq=1024, ldk=1024, ldv=1024, ldy=1024, Mk=20, k=A + 128, v=A + 256)
+    f = dict(kv_heads=4, n_seq=1, max_k=20, **{n + "_head_stride": 256 for n in "qkvy"})
+    assert _call(_attn(**f), y=y, **kw) == B.DP_ERR_INVALID_ARG
+    assert _call(_attn(**f), y=A + 192 * 2, **dict(kw, q=A + 2)) == B.DP_ERR_ALIGN  # (a place of its own: the next check speaks)

@@ -125,3 +125,21 @@ def test_infinite_scores(n, cap, flags):
     rest = torch.ones(n, H, dtype=torch.bool, device="cuda")
     rest[1:4], rest[4, 0] = False, False
     assert ((y.double() - mean).abs() <= tol)[rest].all()
+
+
+@pytest.mark.parametrize("flags", FORMS)
+@pytest.mark.parametrize("order", ["rows", "heads"])
+@pytest.mark.parametrize("KV", [4, 1])
+def test_operands_that_alternate_in_one_buffer(KV, order, flags):
+    """q, k, v and y of a head side by side, [row][head][4][D] or [head][row][4][D]: only y's vectors change."""
+    H, D, n = 4, 72, 210
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    buf = torch.randn(n * H * 4 * D, generator=gen, device="cuda").to(torch.bfloat16)
+    t = buf.view(n, H, 4, D) if order == "rows" else buf.view(H, n, 4, D).transpose(0, 1)
+    before = t.clone()
+    ld, hs = t.stride(0), t.stride(1)
+    at = B.make_attn(H, KV, D, 1, n, n, 0.1, q_head_stride=hs, k_head_stride=hs, v_head_stride=hs, y_head_stride=hs)
+    B.dp_attention(at, t[:, :, 0], ld, n, t[:, :, 1], ld, t[:, :, 2], ld, n, t[:, :, 3], ld, None, flags)
+    want, tol = R.attention(before[:, :, 0], before[:, :KV, 1], before[:, :KV, 2], [n], [n], before[:, :, 3], 0.1)
+    assert ((t[:, :, 3].double() - want).abs() <= tol).all()
+    assert torch.equal(t[:, :, :3], before[:, :, :3])
